@@ -329,6 +329,171 @@ coop_status_t coop_replay(uint64_t *size, uint64_t *cost, uint8_t *kind, uint32_
                           uint64_t *out_cost, uint64_t *out_free, uint32_t *status,
                           void *workspace, size_t workspace_bytes, void *stream);
 
+/* -------------------------------------------------------------------------
+ * Paged pools: the memory that holds the keys and values of the sequences a
+ * model is answering, cut into equal pages.  The pool is described by the
+ * same kind[] array as a snapshot's blocks (one coop_kind_t a page), so the
+ * window search and first fit run on it too.  A sequence's pages are a row of
+ * a block table; a token's slot is page * page_size + its place in the page.
+ *
+ * No call below trusts what device memory holds: page numbers, offsets,
+ * lengths and parents outside their range lead to the documented results and
+ * never to an access outside the arrays described by the counts.  Offset
+ * arrays follow the rules of seg_offsets above except that the last entry may
+ * be smaller than the count it bounds (a padded batch); where they decrease
+ * the results are unspecified.
+ * ---------------------------------------------------------------------- */
+
+/*
+ * coop_page_tables -- brings the block tables of num_requests sequences in
+ * line with their new lengths: first fit over a pool of equal pages, for a
+ * whole batch at once.
+ *
+ * kind[num_pages] (device, coop_kind_t), table[num_requests * max_pages]
+ * (device, row by row: page numbers, -1 where there is none), held[] (device:
+ * how many entries of each row are in use, taken as 0 below and as max_pages
+ * above that range) and lengths[] (device: the tokens each sequence is to
+ * hold) are read; table_out, held_out and kind_out are written.  Each of the
+ * three may be its input (the update is then in place) or must not overlap
+ * any input.  A page is in one row at most.
+ *
+ * A sequence of n tokens needs ceil(n / page_size) pages.
+ *  1. Rows that hold more than they need give back their last pages: these
+ *     become COOP_FREE.
+ *  2. Then the rows that need more take the free pages of lowest number, row
+ *     after row in their order; a page taken becomes `taken`
+ *     (COOP_EVICTABLE or COOP_PINNED).  Once a row cannot have all it needs,
+ *     it and every later row that needs more are refused: they take nothing
+ *     and keep what they had.
+ *  A row whose need exceeds max_pages is refused and keeps what it had; it
+ *  does not hold up the rows after it.
+ * Entries at and past held_out are -1.
+ * status (device u32): bit 0 if a row was refused for want of free pages, bit
+ *   1 if one needed more than max_pages.  free_pages (device u64): the free
+ *   pages left.
+ * workspace: coop_page_tables_workspace_size() bytes (device, 256-byte
+ *   aligned, caller-owned, contents need not be initialised).  num_pages,
+ *   num_requests and max_pages are at most 2^31 - 1 each, and page_size at
+ *   least 1.  With num_requests == 0 the free pages are still counted.
+ */
+coop_status_t coop_page_tables_workspace_size(uint64_t num_pages, uint64_t num_requests,
+                                              size_t *bytes_out);
+
+coop_status_t coop_page_tables(const uint8_t *kind, uint64_t num_pages, const int32_t *table,
+                               uint64_t num_requests, uint64_t max_pages, const int32_t *held,
+                               const uint64_t *lengths, uint64_t page_size, uint8_t taken,
+                               int32_t *table_out, int32_t *held_out, uint8_t *kind_out,
+                               uint32_t *status, uint64_t *free_pages, void *workspace,
+                               size_t workspace_bytes, void *stream);
+
+/*
+ * coop_slot_map -- the slot of every new token.  token_offsets[num_requests +
+ * 1] (device): sequence b's new tokens are [token_offsets[b],
+ * token_offsets[b+1]), the last ones of its lengths[b] tokens.  slots
+ * (device, num_tokens): table[b][pos / page_size] * page_size + pos %
+ * page_size for the token at position pos, and -1 where there is no such
+ * place: the entry is at or past held[b], its page is not below num_pages,
+ * the sequence has more new tokens than it has tokens, or the token lies past
+ * token_offsets[num_requests].
+ */
+coop_status_t coop_slot_map(const int32_t *table, uint64_t num_requests, uint64_t max_pages,
+                            const int32_t *held, const uint64_t *lengths,
+                            const uint64_t *token_offsets, uint64_t num_tokens,
+                            uint64_t page_size, uint64_t num_pages, int64_t *slots,
+                            void *stream);
+
+/* Number types of keys, values and queries. */
+typedef enum {
+    COOP_BF16 = 0,
+    COOP_FP16 = 1,
+    COOP_E4M3 = 2 /* caches only: 1 sign, 4 exponent, 3 mantissa bits, no infinities */
+} coop_type_t;
+
+/* A pool's keys and values.  The row of a page's place and head starts at
+ * page * stride[0] + place * stride[1] + head * stride[2] elements and holds
+ * dim consecutive elements.  k and v are 16-byte aligned, strides are
+ * multiples of 16 bytes; dim is a multiple of 8 (of 16 with COOP_E4M3) and at
+ * most 256.  With COOP_E4M3 an element stands for its value times
+ * k_scale[head] or v_scale[head] (device); otherwise both are NULL.  num_pages
+ * and page_size are at most 2^31 - 1. */
+typedef struct {
+    void *k;
+    void *v;
+    uint64_t k_stride[3];
+    uint64_t v_stride[3];
+    const float *k_scale;
+    const float *v_scale;
+    uint64_t num_pages;
+    uint64_t page_size;
+    uint64_t heads;
+    uint64_t dim;
+    int32_t type; /* coop_type_t */
+} coop_cache_t;
+
+/* Rows of tokens: the row of a token and head starts at token * stride[0] +
+ * head * stride[1] elements (the same rules of alignment as above). */
+typedef struct {
+    const void *data;
+    uint64_t stride[2];
+} coop_rows_t;
+
+/*
+ * coop_cache_write -- writes each token's key and value rows to its slot of
+ * the pool.  k and v have `type` (COOP_BF16 or COOP_FP16), which is the
+ * cache's unless that is COOP_E4M3: then an element is divided by its head's
+ * scale in 32 bits, limited to +-448 and rounded to nearest, ties to even
+ * (NaN stays NaN).  A token whose slot is negative or past the pool is
+ * skipped.  Slots given twice leave one of the rows, or parts of several.
+ */
+coop_status_t coop_cache_write(const coop_rows_t *k, const coop_rows_t *v, int32_t type,
+                               const int64_t *slots, uint64_t num_tokens,
+                               const coop_cache_t *cache, void *stream);
+
+/*
+ * coop_tree_attention -- attention of new tokens over a paged pool and over
+ * one another.  Request b's new tokens are rows [token_offsets[b],
+ * token_offsets[b+1]) of q, k_new and v_new; lengths[b] tokens of it are in
+ * the pool, at the pages of row b of table (max_pages entries; tokens past
+ * max_pages * page_size, and those on a page not below num_pages, do not
+ * count).  Its new tokens form a tree (drafts that share their beginnings):
+ * parents[t] is the request-local number of token t's parent, -1 for a token
+ * that follows the cached ones.  Token t sees all of the cached tokens, itself
+ * and its ancestors, whatever other rows hold.  parents == NULL: each token's
+ * parent is the one before it (a chain: a prompt or a piece of one, or a
+ * single token).  A token whose parent is not -1 or an earlier token of its
+ * request is void: its output is zero, and no other token sees it or what lies
+ * above it.
+ *
+ * For query head h, which reads key/value head h / (q_heads / heads):
+ *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j
+ * over the tokens j that t sees.  Products have 16-bit operands and 32-bit
+ * sums; the softmax's statistics are 32-bit; its weights are rounded to `type`
+ * before they meet the values.
+ *
+ * q, k_new, v_new, out: `type` (COOP_BF16 or COOP_FP16); the cache has the
+ * same type or COOP_E4M3.  q_heads is a multiple of cache->heads.  out
+ * (device, 16-byte aligned): [num_tokens][q_heads][dim], without gaps; rows
+ * past token_offsets[num_requests] are left as they were.
+ * workspace: coop_tree_attention_workspace_size() bytes (device, 256-byte
+ * aligned, caller-owned, contents need not be initialised); two calls in
+ * flight at the same time must not share one.
+ *
+ * Keys and values written to the pool earlier on the same stream are seen.
+ * num_tokens * q_heads and num_requests are at most 2^31 - 1.
+ */
+coop_status_t coop_tree_attention_workspace_size(uint64_t num_requests, uint64_t num_tokens,
+                                                 uint64_t q_heads, uint64_t heads, uint64_t dim,
+                                                 size_t *bytes_out);
+
+coop_status_t coop_tree_attention(const coop_rows_t *q, const coop_rows_t *k_new,
+                                  const coop_rows_t *v_new, int32_t type, uint64_t q_heads,
+                                  uint64_t num_tokens, const uint64_t *token_offsets,
+                                  const int32_t *parents, const coop_cache_t *cache,
+                                  const int32_t *table, uint64_t max_pages,
+                                  const uint64_t *lengths, uint64_t num_requests, float scale,
+                                  void *out, void *workspace, size_t workspace_bytes,
+                                  void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -83,6 +83,7 @@ def load_library():
     lib.coop_window_search_real.argtypes = [vp, vp, vp, u64, vp, u64, vp, vp, u64, vp, vp, vp,
                                             sz, vp]
     lib.coop_window_search_real.restype = ctypes.c_int
+    paged._declare(lib)
     _lib = lib
     return lib
 
@@ -471,9 +472,16 @@ def to_device(pools, device="cuda"):
             u64(pools.seg_offsets), u64(pools.req_sizes), u64(pools.req_offsets))
 
 
-__all__ = ["COOP_EVICTABLE", "COOP_FREE", "COOP_PINNED", "CoopError", "FirstFit",
-           "INFEASIBLE", "LIBRARY", "POLICY_GREEDY", "POLICY_WINDOW", "Replay", "WindowSearch",
-           "first_fit", "first_fit_workspace_size", "load_library", "plan_info",
-           "real_workspace_size", "replay_to_device", "replay_workspace_size", "static_capacity",
-           "to_device", "window_search", "window_search_static", "WindowSearchReal",
-           "workspace_size"]
+from . import paged  # noqa: E402  (it takes the names above)
+from .paged import (CacheWrite, PageTables, SlotMap, TreeAttention, cache_write,  # noqa: E402
+                    page_tables, page_tables_workspace_size, slot_map, tree_attention,
+                    tree_attention_workspace_size)
+
+__all__ = ["COOP_EVICTABLE", "COOP_FREE", "COOP_PINNED", "CacheWrite", "CoopError", "FirstFit",
+           "INFEASIBLE", "LIBRARY", "POLICY_GREEDY", "POLICY_WINDOW", "PageTables", "Replay",
+           "SlotMap", "TreeAttention", "WindowSearch", "cache_write", "first_fit",
+           "first_fit_workspace_size", "load_library", "page_tables",
+           "page_tables_workspace_size", "plan_info", "real_workspace_size", "replay_to_device",
+           "replay_workspace_size", "slot_map", "static_capacity", "to_device", "tree_attention",
+           "tree_attention_workspace_size", "window_search", "window_search_static",
+           "WindowSearchReal", "workspace_size"]

@@ -9,7 +9,9 @@ SOURCES = [os.path.join(PKG, "csrc", "coop_window_search.hip"),
            os.path.join(PKG, "csrc", "coop_window_sub.hip"),
            os.path.join(PKG, "csrc", "coop_first_fit.hip"),
            os.path.join(PKG, "csrc", "coop_replay.hip"),
-           os.path.join(PKG, "csrc", "coop_window_search_real.hip")]
+           os.path.join(PKG, "csrc", "coop_window_search_real.hip"),
+           os.path.join(PKG, "csrc", "coop_pages.hip"),
+           os.path.join(PKG, "csrc", "coop_tree_attention.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIBRARY = os.path.join(PKG, "libcoop.so")
 ARCH = "gfx950"

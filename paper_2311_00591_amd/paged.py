@@ -1,0 +1,390 @@
+"""Paged pools: block tables, slot maps, cache writes and tree attention.
+
+A pool of equal pages holds the keys and values of the sequences that a model
+is answering.  Its pages' kinds are the same uint8 array that window_search and
+first_fit read, so they work on it too.  As in the rest of the package, every
+step runs in the HIP kernels of libcoop.so, calls are asynchronous on torch's
+current stream (or the `stream` argument), and each operator comes as a
+prepared call (a class whose `launch` can be repeated or captured into a graph)
+and as a function.
+
+Caches are tensors [pages, page_size, heads, dim] of bfloat16, float16 or
+float8_e4m3fn, in any order of the first three dimensions in memory (a
+transposed view, or one half of a tensor that holds keys and values together).
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional
+
+import torch
+
+from . import COOP_EVICTABLE, COOP_PINNED, _check, _ptr, load_library
+
+_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
+
+
+class CoopCache(ctypes.Structure):
+    """coop_cache_t."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_stride", ctypes.c_uint64 * 3), ("v_stride", ctypes.c_uint64 * 3),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("num_pages", ctypes.c_uint64), ("page_size", ctypes.c_uint64),
+                ("heads", ctypes.c_uint64), ("dim", ctypes.c_uint64), ("type", ctypes.c_int32)]
+
+
+class CoopRows(ctypes.Structure):
+    """coop_rows_t."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_uint64 * 2)]
+
+
+def _gpu(device):
+    if device.type != "cuda":
+        raise ValueError(f"paged pools are worked on by the GPU; tensors are on {device} "
+                         "(there is no CPU fallback)")
+    return device
+
+
+def _vector(t: torch.Tensor, name: str, dtype, device, *shape) -> torch.Tensor:
+    if t.dtype != dtype and not (dtype == torch.int64 and t.dtype == torch.uint64):
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _strides(t: torch.Tensor, name: str, elements: int, count: int):
+    """The strides of the leading dimensions, of which one of size 1 or a
+    tensor without elements has none that matters."""
+    size, stride = t.shape, t.stride()
+    if t.numel() == 0:
+        return (0,) * count
+    if stride[-1] != 1 and size[-1] != 1:
+        raise ValueError(f"{name}'s last dimension must be contiguous")
+    out = tuple(0 if size[i] == 1 else stride[i] for i in range(count))
+    if any(x % elements for x in out) or t.data_ptr() % 16:
+        raise ValueError(f"{name}'s rows must start at multiples of 16 bytes")
+    return out
+
+
+def _rows(t: torch.Tensor, name: str, dtype, device, tokens, heads, dim) -> CoopRows:
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.shape != (tokens, heads, dim):
+        raise ValueError(f"{name} must have shape {(tokens, heads, dim)}, got {tuple(t.shape)}")
+    return CoopRows(_ptr(t), _strides(t, name, 8, 2))
+
+
+def _cache(k_cache, v_cache, k_scale, v_scale, dtype, device) -> CoopCache:
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
+        raise ValueError("k_cache and v_cache must have one shape [pages, page_size, heads, dim], "
+                         f"got {tuple(k_cache.shape)} and {tuple(v_cache.shape)}")
+    kind = k_cache.dtype
+    if v_cache.dtype != kind or kind not in (dtype, torch.float8_e4m3fn):
+        raise TypeError(f"k_cache and v_cache must both be {dtype} or torch.float8_e4m3fn, got "
+                        f"{kind} and {v_cache.dtype}")
+    if k_cache.device != device or v_cache.device != device:
+        raise ValueError(f"the cache is on {k_cache.device} and {v_cache.device}, expected {device}")
+    pages, page_size, heads, dim = k_cache.shape
+    elements = 8
+    if kind == torch.float8_e4m3fn:
+        elements = 16
+        if k_scale is None or v_scale is None:
+            raise ValueError("a float8_e4m3fn cache needs k_scale and v_scale")
+        _vector(k_scale, "k_scale", torch.float32, device, heads)
+        _vector(v_scale, "v_scale", torch.float32, device, heads)
+    elif k_scale is not None or v_scale is not None:
+        raise ValueError(f"a {kind} cache has no k_scale or v_scale")
+    return CoopCache(_ptr(k_cache), _ptr(v_cache), _strides(k_cache, "k_cache", elements, 3),
+                     _strides(v_cache, "v_cache", elements, 3),
+                     None if k_scale is None else k_scale.data_ptr(),
+                     None if v_scale is None else v_scale.data_ptr(),
+                     pages, page_size, heads, dim, _TYPES[kind])
+
+
+def _workspace(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+    if workspace is None:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+    if workspace.device != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous memory on {device}")
+    if workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"workspace holds {workspace.numel() * workspace.element_size()} bytes, "
+                         f"needs {need}")
+    return workspace
+
+
+class _Call:
+    """A prepared call: the C function, its arguments (all but the stream) and
+    the tensors that it uses, which it keeps alive.  `made` are those that it
+    allocated itself."""
+
+    def _prepare(self, device, fn, args, made):
+        self.device, self._fn, self._args, self._made = device, fn, args, made
+
+    def launch(self, stream: Optional[int] = None) -> None:
+        """Enqueues the call on `stream` (default: torch's current stream of
+        the tensors' device)."""
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device).cuda_stream
+        elif stream != torch.cuda.current_stream(self.device).cuda_stream:
+            # memory from torch's allocator is not reused before that stream is done with it
+            other = torch.cuda.ExternalStream(stream, self.device)
+            for t in self._made:
+                t.record_stream(other)
+        if torch.cuda.current_device() == self.device.index:
+            _check(self._fn(*self._args, stream))
+        else:
+            with torch.cuda.device(self.device):
+                _check(self._fn(*self._args, stream))
+
+
+def page_tables_workspace_size(num_pages: int, num_requests: int) -> int:
+    """Device workspace bytes coop_page_tables needs."""
+    out = ctypes.c_size_t(0)
+    _check(load_library().coop_page_tables_workspace_size(int(num_pages), int(num_requests),
+                                                          ctypes.byref(out)))
+    return out.value
+
+
+class PageTables(_Call):
+    """A prepared coop_page_tables call: brings the block tables of a batch of
+    sequences in line with their new lengths.
+
+    kind: uint8 [pages] (0 free, 1 evictable, 2 pinned); table: int32
+    [requests, columns], page numbers; held: int32 [requests], the entries in
+    use of each row; lengths: int64 [requests], the tokens that each sequence is
+    to hold.  Rows that hold more pages than ceil(length / page_size) give their
+    last ones back; then rows that need more take the lowest free pages, in the
+    rows' order, which become `taken`.  Once a row cannot have all that it
+    needs, it and every later one that needs more keep what they had.
+
+    Results: `table`, `held`, `kind` (new tensors; with out=(table, held, kind)
+    written there, and these may be the inputs themselves), `status` (int32
+    [1]: bit 0, a row was refused for want of free pages; bit 1, one needs more
+    than a row has columns) and `free` (int64 [1], free pages left)."""
+
+    def __init__(self, kind, table, held, lengths, page_size: int, *, taken: int = COOP_PINNED,
+                 out=None, workspace: Optional[torch.Tensor] = None):
+        device = _gpu(kind.device)
+        if kind.dim() != 1 or table.dim() != 2:
+            raise ValueError("kind must have shape [pages] and table [requests, columns], got "
+                             f"{tuple(kind.shape)} and {tuple(table.shape)}")
+        pages, (rows, cols) = kind.numel(), table.shape
+        _vector(kind, "kind", torch.uint8, device, pages)
+        _vector(table, "table", torch.int32, device, rows, cols)
+        _vector(held, "held", torch.int32, device, rows)
+        _vector(lengths, "lengths", torch.int64, device, rows)
+        if page_size < 1:
+            raise ValueError(f"page_size must be at least 1, got {page_size}")
+        if taken not in (COOP_EVICTABLE, COOP_PINNED):
+            raise ValueError(f"taken must be COOP_EVICTABLE or COOP_PINNED, got {taken}")
+        made = []
+        if out is None:
+            out = made = [torch.empty_like(t) for t in (table, held, kind)]
+        self.table = _vector(out[0], "out[0]", torch.int32, device, rows, cols)
+        self.held = _vector(out[1], "out[1]", torch.int32, device, rows)
+        self.kind = _vector(out[2], "out[2]", torch.uint8, device, pages)
+        words = torch.empty(2, dtype=torch.int64, device=device)
+        self.free, self.status = words[:1], words[1:].view(torch.int32)[:1]
+        self.workspace = _workspace(workspace, page_tables_workspace_size(pages, rows), device)
+        self._inputs = (kind, table, held, lengths)
+        self._prepare(device, load_library().coop_page_tables,
+                      (_ptr(kind), pages, _ptr(table), rows, cols, _ptr(held), _ptr(lengths),
+                       page_size, taken, _ptr(self.table), _ptr(self.held), _ptr(self.kind),
+                       self.status.data_ptr(), self.free.data_ptr(), self.workspace.data_ptr(),
+                       self.workspace.numel() * self.workspace.element_size()),
+                      [*made, words, self.workspace])
+
+    def __call__(self, stream: Optional[int] = None):
+        self.launch(stream)
+        return self.table, self.held, self.kind, self.status, self.free
+
+
+def page_tables(kind, table, held, lengths, page_size: int, *, taken: int = COOP_PINNED, out=None,
+                workspace: Optional[torch.Tensor] = None, stream: Optional[int] = None):
+    """One PageTables call; returns (table, held, kind, status, free)."""
+    return PageTables(kind, table, held, lengths, page_size, taken=taken, out=out,
+                      workspace=workspace)(stream)
+
+
+class SlotMap(_Call):
+    """A prepared coop_slot_map call: the slot (page * page_size + place) of
+    each of num_tokens new tokens.  token_offsets: int64 [requests + 1];
+    sequence b's new tokens are the last token_offsets[b+1] - token_offsets[b]
+    of its lengths[b].  -1 where a token has no place.  Result: `slots`, int64
+    [num_tokens]."""
+
+    def __init__(self, table, held, lengths, token_offsets, num_tokens: int, page_size: int,
+                 num_pages: int, out: Optional[torch.Tensor] = None):
+        device = _gpu(table.device)
+        if table.dim() != 2:
+            raise ValueError(f"table must have shape [requests, columns], got {tuple(table.shape)}")
+        rows, cols = table.shape
+        _vector(table, "table", torch.int32, device, rows, cols)
+        _vector(held, "held", torch.int32, device, rows)
+        _vector(lengths, "lengths", torch.int64, device, rows)
+        _vector(token_offsets, "token_offsets", torch.int64, device, rows + 1)
+        if num_tokens < 0 or page_size < 1 or num_pages < 0:
+            raise ValueError(f"num_tokens {num_tokens}, page_size {page_size} and num_pages "
+                             f"{num_pages} must be at least 0, 1 and 0")
+        made = []
+        if out is None:
+            out = torch.empty(num_tokens, dtype=torch.int64, device=device)
+            made = [out]
+        self.slots = _vector(out, "out", torch.int64, device, num_tokens)
+        self._inputs = (table, held, lengths, token_offsets)
+        self._prepare(device, load_library().coop_slot_map,
+                      (_ptr(table), rows, cols, _ptr(held), _ptr(lengths),
+                       token_offsets.data_ptr(), num_tokens, page_size, num_pages,
+                       _ptr(self.slots)), made)
+
+    def __call__(self, stream: Optional[int] = None) -> torch.Tensor:
+        self.launch(stream)
+        return self.slots
+
+
+def slot_map(table, held, lengths, token_offsets, num_tokens: int, page_size: int, num_pages: int,
+             *, out: Optional[torch.Tensor] = None, stream: Optional[int] = None) -> torch.Tensor:
+    """One SlotMap call; returns int64 [num_tokens]."""
+    return SlotMap(table, held, lengths, token_offsets, num_tokens, page_size, num_pages,
+                   out)(stream)
+
+
+class CacheWrite(_Call):
+    """A prepared coop_cache_write call: rows of keys and values ([tokens,
+    heads, dim], bfloat16 or float16) to their slots of the pool (int64
+    [tokens]; tokens without a slot in the pool are skipped, and slots must
+    differ).  A float8_e4m3fn cache stores them divided by their head's scale
+    (float32 [heads]), limited to +-448."""
+
+    def __init__(self, k, v, slots, k_cache, v_cache, *, k_scale=None, v_scale=None):
+        device = _gpu(k.device)
+        if k.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"k must be torch.bfloat16 or torch.float16, got {k.dtype}")
+        if k.dim() != 3:
+            raise ValueError(f"k must have shape [tokens, heads, dim], got {tuple(k.shape)}")
+        cache = _cache(k_cache, v_cache, k_scale, v_scale, k.dtype, device)
+        n = k.shape[0]
+        rows = [_rows(t, name, k.dtype, device, n, cache.heads, cache.dim)
+                for t, name in ((k, "k"), (v, "v"))]
+        _vector(slots, "slots", torch.int64, device, n)
+        self.k_cache, self.v_cache = k_cache, v_cache
+        self._inputs = (k, v, slots, k_scale, v_scale)
+        self._prepare(device, load_library().coop_cache_write,
+                      (*rows, _TYPES[k.dtype], _ptr(slots), n, cache), [])
+
+    def __call__(self, stream: Optional[int] = None):
+        self.launch(stream)
+        return self.k_cache, self.v_cache
+
+
+def cache_write(k, v, slots, k_cache, v_cache, *, k_scale=None, v_scale=None,
+                stream: Optional[int] = None):
+    """One CacheWrite call; returns (k_cache, v_cache), written in place."""
+    return CacheWrite(k, v, slots, k_cache, v_cache, k_scale=k_scale, v_scale=v_scale)(stream)
+
+
+def tree_attention_workspace_size(num_requests: int, num_tokens: int, q_heads: int, heads: int,
+                                  dim: int) -> int:
+    """Device workspace bytes coop_tree_attention needs."""
+    out = ctypes.c_size_t(0)
+    _check(load_library().coop_tree_attention_workspace_size(
+        int(num_requests), int(num_tokens), int(q_heads), int(heads), int(dim), ctypes.byref(out)))
+    return out.value
+
+
+class TreeAttention(_Call):
+    """A prepared coop_tree_attention call: attention of new tokens over the
+    cached tokens of their requests and over one another.
+
+    q [tokens, q_heads, dim], k and v [tokens, heads, dim] (bfloat16 or
+    float16): the new tokens; request b's are token_offsets[b] to
+    token_offsets[b+1] (int64 [requests + 1]).  lengths (int64 [requests]): the
+    tokens in the pool, on the pages of table's rows (int32 [requests,
+    columns]).  parents (int32 [tokens]): the request-local number of each
+    token's parent in its request's tree, -1 where it follows the cached tokens
+    directly; a token sees the cached tokens, its ancestors and itself.
+    parents=None: a chain, each token the parent of the next (a prompt or a
+    piece of one; single tokens).  A parent that is neither -1 nor an earlier
+    token makes its token void: a zero row, which no other token sees.
+    scale: of the products, dim ** -0.5 by default.  Result: `out` [tokens,
+    q_heads, dim] of q's type."""
+
+    def __init__(self, q, k, v, k_cache, v_cache, table, lengths, token_offsets, parents=None, *,
+                 scale: Optional[float] = None, k_scale=None, v_scale=None,
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+        device = _gpu(q.device)
+        if q.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError(f"q must be torch.bfloat16 or torch.float16, got {q.dtype}")
+        if q.dim() != 3 or table.dim() != 2:
+            raise ValueError("q must have shape [tokens, q_heads, dim] and table [requests, "
+                             f"columns], got {tuple(q.shape)} and {tuple(table.shape)}")
+        cache = _cache(k_cache, v_cache, k_scale, v_scale, q.dtype, device)
+        n, q_heads, dim = q.shape
+        if cache.heads == 0 or q_heads == 0 or q_heads % cache.heads:
+            raise ValueError(f"{q_heads} query heads cannot share {cache.heads} key/value heads")
+        requests, cols = table.shape
+        rows = [_rows(t, name, q.dtype, device, n, heads, cache.dim)
+                for t, name, heads in ((q, "q", q_heads), (k, "k", cache.heads),
+                                       (v, "v", cache.heads))]
+        _vector(table, "table", torch.int32, device, requests, cols)
+        _vector(lengths, "lengths", torch.int64, device, requests)
+        _vector(token_offsets, "token_offsets", torch.int64, device, requests + 1)
+        if parents is not None:
+            _vector(parents, "parents", torch.int32, device, n)
+        made = []
+        if out is None:
+            out = torch.empty((n, q_heads, dim), dtype=q.dtype, device=device)
+            made.append(out)
+        self.out = _vector(out, "out", q.dtype, device, n, q_heads, dim)
+        need = tree_attention_workspace_size(requests, n, q_heads, cache.heads, dim)
+        if workspace is None:
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+            made.append(workspace)
+        self.workspace = _workspace(workspace, need, device)
+        self._inputs = (q, k, v, k_cache, v_cache, table, lengths, token_offsets, parents, k_scale,
+                        v_scale)
+        self._prepare(device, load_library().coop_tree_attention,
+                      (*rows, _TYPES[q.dtype], q_heads, n, token_offsets.data_ptr(),
+                       None if parents is None else _ptr(parents), cache, _ptr(table), cols,
+                       _ptr(lengths), requests, dim ** -0.5 if scale is None else float(scale),
+                       _ptr(self.out), self.workspace.data_ptr(),
+                       self.workspace.numel() * self.workspace.element_size()), made)
+
+    def __call__(self, stream: Optional[int] = None) -> torch.Tensor:
+        self.launch(stream)
+        return self.out
+
+
+def tree_attention(q, k, v, k_cache, v_cache, table, lengths, token_offsets, parents=None, *,
+                   scale: Optional[float] = None, k_scale=None, v_scale=None,
+                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                   stream: Optional[int] = None) -> torch.Tensor:
+    """One TreeAttention call; returns [tokens, q_heads, dim]."""
+    return TreeAttention(q, k, v, k_cache, v_cache, table, lengths, token_offsets, parents,
+                         scale=scale, k_scale=k_scale, v_scale=v_scale, out=out,
+                         workspace=workspace)(stream)
+
+
+def _declare(lib) -> None:
+    """The C signatures of the functions above."""
+    u64, vp, sz, i32 = ctypes.c_uint64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
+    rows, cache, size_out = (ctypes.POINTER(CoopRows), ctypes.POINTER(CoopCache),
+                             ctypes.POINTER(sz))
+    lib.coop_page_tables_workspace_size.argtypes = [u64, u64, size_out]
+    lib.coop_page_tables.argtypes = [vp, u64, vp, u64, u64, vp, vp, u64, ctypes.c_uint8, vp, vp,
+                                     vp, vp, vp, vp, sz, vp]
+    lib.coop_slot_map.argtypes = [vp, u64, u64, vp, vp, vp, u64, u64, u64, vp, vp]
+    lib.coop_cache_write.argtypes = [rows, rows, i32, vp, u64, cache, vp]
+    lib.coop_tree_attention_workspace_size.argtypes = [u64, u64, u64, u64, u64, size_out]
+    lib.coop_tree_attention.argtypes = [rows, rows, rows, i32, u64, u64, vp, vp, cache, vp, u64,
+                                        vp, u64, ctypes.c_float, vp, vp, sz, vp]
+    for name in ("coop_page_tables_workspace_size", "coop_page_tables", "coop_slot_map",
+                 "coop_cache_write", "coop_tree_attention_workspace_size", "coop_tree_attention"):
+        getattr(lib, name).restype = ctypes.c_int
