@@ -1,9 +1,40 @@
 // Attention of a tree of new tokens over a paged pool, for gfx950.
 //
-// One wavefront a new token and query head: it walks the request's cached keys
-// and then the token's ancestors, with the running maximum m and sum l of the
-// softmax:  m' = max(m, s),  l' = l e^(m - m') + e^(s - m'),
-// o' = o e^(m - m') + e^(s - m') v,  out = o / l.
+// The mathematics.  For one request and key/value head, the rows are its new
+// tokens times the query heads that share the head (row r: token r / G, head
+// h G + r % G), and all rows meet the same keys.  A tile of keys is taken in
+// with the running maximum m and sum l of the softmax (in powers of two, the
+// scale times log2 e applied to the 32-bit product):
+//   S = K Q^T,  m' = max(m, max S),  P = 2^(S - m'),
+//   l' = l 2^(m - m') + sum P,  O' = O 2^(m - m') + V^T P,
+// and the parts (m, l, O) of separate key ranges join by the same rule.
+//
+// What bounds it.  A key's row and a value's row (4 dim bytes) meet up to
+// G T rows, 4 dim products each: below about 250 rows the pool's bytes
+// bound the call, above that the matrix instructions.
+//
+// The work.  A workgroup of four wavefronts takes an item: 32 kRowWaves rows of
+// one request and head, and a range of its keys.  kRowWaves wavefronts share
+// a tile of keys in LDS, 32 rows each; 4 / kRowWaves groups take tiles in
+// turn and are joined at the end, so that few rows still keep four wavefronts'
+// loads under way.  Keys are cut into ranges where the requests alone would
+// leave compute units idle; the parts of cut ranges go to the workspace and a
+// second kernel joins them.  A small kernel ahead of both reads the lengths,
+// which only the device knows, and lists the items.
+//
+// Operands.  Products are 32x32x16 matrix instructions with the keys as the
+// rows of the first one: its result then holds, in each lane, one query row
+// and keys 8 i + 4 (lane / 32) + 0..3, which is the layout that the second
+// product's operand needs when the values are read in the same order of keys.
+// The weights never leave the registers.  Values are read from LDS by the
+// transposing load, four keys of one column a lane.  Chunks of 16 bytes are
+// permuted within a row of LDS so that the keys' 16-byte reads and the
+// values' transposing reads touch every bank once.
+//
+// Tree.  A lane's row knows its token; the tokens that it sees in a tile of
+// 32 or 64 new tokens are a word of bits, collected by walking up from the
+// token.  Tiles of new tokens are taken from the last to the first, so each
+// walk goes on where the one before it stopped.
 
 #include <hip/hip_runtime.h>
 
@@ -14,6 +45,30 @@
 
 namespace {
 
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kRows = 32;            // rows of a wavefront
+constexpr uint32_t kParentsInLds = 512;   // trees up to this size are walked in LDS
+constexpr uint32_t kPlanThreads = 1024;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLowest = -__builtin_inff();
+
+struct Item {  // rows [32 kRowWaves rt, ...) of a request and head, tiles [first, last)
+    uint32_t request, row_tile, head, first, last;
+    uint32_t part;  // where its result goes in the workspace; kWhole: to the output
+    uint32_t pad[2];
+};
+constexpr uint32_t kWhole = ~0u;
+
+struct Join {  // rows whose keys were cut into `parts` ranges
+    uint32_t request, row_tile, head, parts, first;
+    uint32_t pad[3];
+};
+
+struct Head {
+    uint32_t items, joins;
+    uint32_t pad[6];
+};
+
 struct Args {
     coop_rows_t q, k, v;
     coop_cache_t cache;
@@ -23,99 +78,734 @@ struct Args {
     const uint64_t* lengths;
     uint16_t* out;
     uint64_t tokens;
-    uint32_t requests, max_pages, q_heads, type;
+    uint32_t requests, max_pages, q_heads, group;
     float scale;
+    // the plan and the workspace
+    uint32_t tile_keys, row_tile_rows, target, least, chunk_multiple, max_items, part_rows;
+    Head* head;
+    Item* items;
+    Join* joins;
+    float* part_out;   // [part][part_rows][kDim]
+    float2* part_sum;  // [part][part_rows] (m, l)
 };
 
-__device__ __forceinline__ uint16_t from_float(float x, uint32_t type) {
-    if (type == COOP_FP16) return __builtin_bit_cast(uint16_t, static_cast<_Float16>(x));
-    return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x));
+// ---------------------------------------------------------------------------
+// The plan
+// ---------------------------------------------------------------------------
+
+struct Extent {
+    uint64_t first;    // first new token
+    uint32_t tokens;   // new tokens
+    uint32_t cached;   // cached tokens that the table can name
+};
+
+__device__ __forceinline__ Extent extent(const Args& a, uint32_t b) {
+    Extent e;
+    const uint64_t o0 = a.offsets[b], o1 = min(a.offsets[b + 1], a.tokens);
+    e.first = o0;
+    e.tokens = o0 < o1 ? static_cast<uint32_t>(o1 - o0) : 0u;
+    const uint64_t most = static_cast<uint64_t>(a.max_pages) * a.cache.page_size;
+    e.cached = a.cache.num_pages ? static_cast<uint32_t>(min(a.lengths[b], most)) : 0u;
+    return e;
 }
 
-// One element of the cache as a 32-bit number, without its head's scale.
-__device__ __forceinline__ float cached(const void* base, uint64_t at, int32_t cache_type) {
-    if (cache_type == COOP_E4M3)
-        return __builtin_amdgcn_cvt_f32_fp8(static_cast<const uint8_t*>(base)[at], 0);
-    return coop_pages::to_float(static_cast<const uint16_t*>(base)[at], cache_type);
+__device__ __forceinline__ uint32_t ceil_div(uint32_t x, uint32_t y) { return (x + y - 1) / y; }
+
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
+    for (uint32_t d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
 }
 
-__global__ __launch_bounds__(64) void tree_attention_kernel(Args a) {
-    const uint32_t lane = threadIdx.x, dim = static_cast<uint32_t>(a.cache.dim);
-    const uint64_t t = blockIdx.x / a.q_heads;
-    const uint32_t hq = static_cast<uint32_t>(blockIdx.x - t * a.q_heads);
-    const uint32_t h = hq / (a.q_heads / static_cast<uint32_t>(a.cache.heads));
-    uint32_t lo = 0, hi = a.requests + 1;
-    while (lo < hi) {
-        const uint32_t mid = (lo + hi) >> 1;
-        if (a.offsets[mid] > t) hi = mid;
-        else lo = mid + 1;
+// Lists the items.  All ranges are `chunk` tiles long, a length that gives
+// about `target` of them when the keys are spread evenly: with W tiles in all,
+// chunk >= W / target, so the rows that are cut make at most 2 target parts.
+__global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
+    __shared__ uint64_t part[kPlanThreads / 64][3];
+    __shared__ uint32_t item_base[kPlanThreads + 1], cut_base[kPlanThreads], join_base[kPlanThreads + 1];
+    __shared__ uint32_t row_tiles_of[kPlanThreads], tiles_of[kPlanThreads];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u, w = tid >> 6;
+    const uint32_t heads = static_cast<uint32_t>(a.cache.heads);
+    uint64_t work = 0;
+    for (uint32_t b = tid; b < a.requests; b += kPlanThreads) {
+        const Extent e = extent(a, b);
+        const uint64_t rt = (static_cast<uint64_t>(e.tokens) * a.group + a.row_tile_rows - 1) / a.row_tile_rows;
+        work += rt * heads * (ceil_div(e.cached, a.tile_keys) + ceil_div(e.tokens, a.tile_keys));
     }
-    if (lo == 0 || lo > a.requests) return;
-    const uint32_t b = lo - 1;
-    const uint64_t first = a.offsets[b];
-    const int64_t self = static_cast<int64_t>(t - first);
-    float q[4], o[4] = {0, 0, 0, 0}, m = -__builtin_inff(), l = 0;
-    const uint16_t* const qr =
-        static_cast<const uint16_t*>(a.q.data) + t * a.q.stride[0] + hq * a.q.stride[1];
-    for (uint32_t i = 0; i < 4; ++i)
-        q[i] = lane + 64 * i < dim ? coop_pages::to_float(qr[lane + 64 * i], a.type) : 0.f;
-    const bool is_void = a.parents && (a.parents[t] < -1 || a.parents[t] >= self);
+    work = wave_sum(work);
+    if (lane == 0) part[w][0] = work;
+    __syncthreads();
+    work = 0;
+    for (uint32_t i = 0; i < kPlanThreads / 64; ++i) work += part[i][0];
+    uint64_t chunk64 = max((work + a.target - 1) / a.target, static_cast<uint64_t>(a.least));
+    chunk64 = (chunk64 + a.chunk_multiple - 1) / a.chunk_multiple * a.chunk_multiple;
+    const uint32_t chunk = static_cast<uint32_t>(min(chunk64, static_cast<uint64_t>(1u << 30)));
+    uint32_t items0 = 0, cuts0 = 0, joins0 = 0;  // of the requests before this batch
+    for (uint32_t b0 = 0; b0 < a.requests; b0 += kPlanThreads) {
+        const uint32_t b = b0 + tid;
+        uint32_t tiles = 0, rt = 0;
+        if (b < a.requests) {
+            const Extent e = extent(a, b);
+            rt = static_cast<uint32_t>(
+                (static_cast<uint64_t>(e.tokens) * a.group + a.row_tile_rows - 1) / a.row_tile_rows);
+            tiles = ceil_div(e.cached, a.tile_keys) + ceil_div(e.tokens, a.tile_keys);
+        }
+        const uint32_t pairs = rt * heads, ranges = ceil_div(tiles, chunk);
+        const uint64_t mine[3] = {static_cast<uint64_t>(pairs) * ranges,
+                                  ranges > 1 ? static_cast<uint64_t>(pairs) * ranges : 0,
+                                  ranges > 1 ? pairs : 0};
+        uint64_t sum[3], all[3];
+        for (int k = 0; k < 3; ++k) {
+            sum[k] = mine[k];
+            for (uint32_t d = 1; d < 64; d <<= 1) {
+                const uint64_t up = __shfl_up(sum[k], d, 64);
+                if (lane >= d) sum[k] += up;
+            }
+        }
+        __syncthreads();
+        if (lane == 63)
+            for (int k = 0; k < 3; ++k) part[w][k] = sum[k];
+        __syncthreads();
+        for (int k = 0; k < 3; ++k) {
+            all[k] = 0;
+            for (uint32_t i = 0; i < kPlanThreads / 64; ++i) {
+                if (i < w) sum[k] += part[i][k];
+                all[k] += part[i][k];
+            }
+        }
+        item_base[tid] = static_cast<uint32_t>(min(sum[0] - mine[0], static_cast<uint64_t>(kWhole)));
+        cut_base[tid] = static_cast<uint32_t>(sum[1] - mine[1]);
+        join_base[tid] = static_cast<uint32_t>(sum[2] - mine[2]);
+        row_tiles_of[tid] = rt;
+        tiles_of[tid] = tiles;
+        if (tid == kPlanThreads - 1) {
+            item_base[kPlanThreads] = static_cast<uint32_t>(min(sum[0], static_cast<uint64_t>(kWhole)));
+            join_base[kPlanThreads] = static_cast<uint32_t>(sum[2]);
+        }
+        __syncthreads();
+        const uint32_t n = min(item_base[kPlanThreads], a.max_items - items0);
+        for (uint32_t i = tid; i < n; i += kPlanThreads) {
+            uint32_t lo = 0, hi = kPlanThreads;  // the last request whose items start at or before i
+            while (hi - lo > 1) {
+                const uint32_t mid = (lo + hi) >> 1;
+                if (item_base[mid] <= i) lo = mid;
+                else hi = mid;
+            }
+            const uint32_t j = i - item_base[lo], p = row_tiles_of[lo] * heads;
+            const uint32_t c = j / p, pair = j - c * p;
+            const uint32_t t = tiles_of[lo], r = ceil_div(t, chunk);
+            Item it;
+            it.request = b0 + lo;
+            it.row_tile = pair / heads;
+            it.head = pair - it.row_tile * heads;
+            it.first = c * chunk;
+            it.last = min(t, it.first + chunk);
+            it.part = r > 1 ? cuts0 + cut_base[lo] + pair * r + c : kWhole;
+            it.pad[0] = it.pad[1] = 0;
+            a.items[items0 + i] = it;
+        }
+        for (uint32_t i = tid; i < join_base[kPlanThreads]; i += kPlanThreads) {
+            uint32_t lo = 0, hi = kPlanThreads;
+            while (hi - lo > 1) {
+                const uint32_t mid = (lo + hi) >> 1;
+                if (join_base[mid] <= i) lo = mid;
+                else hi = mid;
+            }
+            const uint32_t pair = i - join_base[lo], r = ceil_div(tiles_of[lo], chunk);
+            Join jn;
+            jn.request = b0 + lo;
+            jn.row_tile = pair / heads;
+            jn.head = pair - jn.row_tile * heads;
+            jn.parts = r;
+            jn.first = cuts0 + cut_base[lo] + pair * r;
+            jn.pad[0] = jn.pad[1] = jn.pad[2] = 0;
+            a.joins[joins0 + i] = jn;
+        }
+        items0 += n;
+        cuts0 += static_cast<uint32_t>(all[1]);
+        joins0 += join_base[kPlanThreads];
+        __syncthreads();
+    }
+    if (tid == 0) {
+        a.head->items = items0;
+        a.head->joins = joins0;
+    }
+}
 
-    auto visit = [&](const float* kx, const float* vx, float ks, float vs) {
-        float s = 0;
-        for (uint32_t i = 0; i < 4; ++i) s += q[i] * kx[i];
-        for (uint32_t d = 32; d; d >>= 1) s += __shfl_xor(s, d, 64);
-        s *= a.scale * ks;
-        const float top = fmaxf(m, s);
-        const float was = m == top ? 1.f : __expf(m - top);
-        const float p = __expf(s - top);
-        l = l * was + p;
-        for (uint32_t i = 0; i < 4; ++i) o[i] = o[i] * was + p * vs * vx[i];
-        m = top;
+// ---------------------------------------------------------------------------
+// Number types
+// ---------------------------------------------------------------------------
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+struct Bf16 {
+    typedef __bf16 Vec8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 Vec2 __attribute__((ext_vector_type(2)));
+    static constexpr uint32_t kExponent = 0x7f80u;
+    static __device__ __forceinline__ f32x16 mfma(u32x4 x, u32x4 y, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Vec8, x),
+                                                       __builtin_bit_cast(Vec8, y), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) {
+        const Vec2 v = {static_cast<__bf16>(x), static_cast<__bf16>(y)};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+    static __device__ __forceinline__ float value(uint16_t bits) {
+        return __uint_as_float(static_cast<uint32_t>(bits) << 16);
+    }
+    template <bool kUpper>
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t word) {
+        return __builtin_bit_cast(uint32_t,
+                                  __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(word, 1.f, kUpper));
+    }
+};
+
+struct Fp16 {
+    typedef _Float16 Vec8 __attribute__((ext_vector_type(8)));
+    typedef _Float16 Vec2 __attribute__((ext_vector_type(2)));
+    static constexpr uint32_t kExponent = 0x7c00u;
+    static __device__ __forceinline__ f32x16 mfma(u32x4 x, u32x4 y, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Vec8, x),
+                                                      __builtin_bit_cast(Vec8, y), c, 0, 0, 0);
+    }
+    static __device__ __forceinline__ uint32_t pack(float x, float y) {
+        const Vec2 v = {static_cast<_Float16>(x), static_cast<_Float16>(y)};
+        return __builtin_bit_cast(uint32_t, v);
+    }
+    static __device__ __forceinline__ float value(uint16_t bits) {
+        return static_cast<float>(__builtin_bit_cast(_Float16, bits));
+    }
+    template <bool kUpper>
+    static __device__ __forceinline__ uint32_t from_e4m3(uint32_t word) {
+        return __builtin_bit_cast(uint32_t,
+                                  __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(word, 1.f, kUpper));
+    }
+};
+
+// ---------------------------------------------------------------------------
+// The attention kernel
+// ---------------------------------------------------------------------------
+
+template <class T, bool kE4M3, uint32_t kDim, uint32_t kRowWaves>
+struct Shape {
+    static constexpr uint32_t kGroups = 4 / kRowWaves;
+    static constexpr uint32_t kKeys = kRowWaves == 1 ? 32 : 64;  // of a tile
+    static constexpr uint32_t kGroupThreads = 64 * kRowWaves;
+    static constexpr uint32_t kChunks = kDim / 8;  // 16-byte chunks of a row in LDS
+    static constexpr uint32_t kLoads = kKeys * kChunks / kGroupThreads;      // a thread's, a tile
+    static constexpr uint32_t kLoads8 = kLoads / 2;                          // with 8-bit rows
+    static constexpr uint32_t kTileBytes = kKeys * kDim * 2;
+    static constexpr uint32_t kSTiles = kKeys / 32;
+    static constexpr uint32_t kDTiles = kDim / 32;
+    static constexpr uint32_t kBytes = kGroups * 2 * kTileBytes;
+    static_assert(kLoads8 >= 1, "a thread has a load of every kind");
+};
+
+// Where chunk c of row r lies in its row.
+template <uint32_t kDim>
+__device__ __forceinline__ uint32_t key_chunk(uint32_t r, uint32_t c) {
+    return kDim == 64 ? c ^ ((r >> 1) & 7u) : c ^ (r & 15u);
+}
+template <uint32_t kDim>
+__device__ __forceinline__ uint32_t value_chunk(uint32_t r, uint32_t c) {
+    return kDim == 64 ? c ^ (((r >> 1) & 1u) << 2) : c ^ ((r & 3u) << 2);
+}
+
+struct RowAt {  // where a tile's key and value rows are in memory
+    const uint8_t* k;
+    const uint8_t* v;
+};
+
+template <class T, bool kE4M3, uint32_t kDim, uint32_t kRowWaves>
+__global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_kernel(Args a) {
+    using S = Shape<T, kE4M3, kDim, kRowWaves>;
+    constexpr uint32_t kKeys = S::kKeys, kLoads = S::kLoads, kLoads8 = S::kLoads8;
+    __shared__ __align__(16) uint8_t tiles[S::kBytes];
+    __shared__ RowAt rows_at[4][kKeys];           // one copy a wavefront
+    __shared__ int32_t tree[kParentsInLds];
+    __shared__ uint16_t weights[4][32][kRows];    // only for values that are not finite
+    __shared__ uint32_t odd[4];                   // whether a wavefront stored such values
+    __shared__ float joined[4][kRows][2];
+
+    if (blockIdx.x >= a.head->items) return;
+    const Item item = a.items[blockIdx.x];
+    const uint32_t tid = threadIdx.x, lane = tid & 63u;
+    const uint32_t w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t group = w / kRowWaves, row_wave = w % kRowWaves;
+    const uint32_t gtid = tid - group * S::kGroupThreads;
+    const uint32_t n = lane & 31u, hi = lane >> 5;
+    const uint32_t dim = static_cast<uint32_t>(a.cache.dim);
+    const uint32_t page_size = static_cast<uint32_t>(a.cache.page_size);
+    const Extent e = extent(a, item.request);
+    const uint32_t rows = e.tokens * a.group;
+    const uint32_t row0 = item.row_tile * (kRows * kRowWaves);
+    const uint32_t row = row0 + row_wave * kRows + n;
+    const bool row_lives = row < rows;
+    const uint32_t token = row / a.group, qh = item.head * a.group + row % a.group;
+
+    uint8_t* const key_tile = tiles + group * 2 * S::kTileBytes;
+    uint8_t* const value_tile = key_tile + S::kTileBytes;
+
+    // tiles of cached keys, then tiles of new tokens from the last that any of
+    // these rows can see to the first
+    const uint32_t cached_tiles = ceil_div(e.cached, kKeys);
+    const uint32_t last_token = (min(rows, row0 + kRows * kRowWaves) - 1) / a.group;
+    const uint32_t new_tiles = last_token / kKeys + 1;
+    const uint32_t first = item.first, last = min(item.last, cached_tiles + new_tiles);
+
+    const bool in_lds = a.parents && e.tokens <= kParentsInLds && last > cached_tiles;
+    if (in_lds)
+        for (uint32_t i = tid; i < e.tokens; i += kThreads) tree[i] = a.parents[e.first + i];
+    __syncthreads();
+    const int32_t* const parents = a.parents ? a.parents + e.first : nullptr;
+    auto parent_of = [&](int32_t i) { return in_lds ? tree[i] : parents[i]; };
+
+    // the row's place on its way up: a token that it sees, and that one's parent
+    int32_t at = -1, up = -1;
+    if (row_lives && last > cached_tiles) {
+        at = static_cast<int32_t>(token);
+        up = at - 1;
+        if (parents) {
+            up = parent_of(at);
+            if (up < -1 || up >= at) at = -1;
+        }
+    }
+    auto climb = [&]() {
+        const int32_t next = up;
+        if (next < 0) {
+            at = -1;
+            return;
+        }
+        const int32_t above = parent_of(next);
+        at = above < -1 || above >= next ? -1 : next;
+        up = above;
     };
 
-    if (!is_void) {
-        const uint64_t most = static_cast<uint64_t>(a.max_pages) * a.cache.page_size;
-        const uint64_t n = a.lengths[b] < most ? a.lengths[b] : most;
-        const float ks = a.cache.k_scale ? a.cache.k_scale[h] : 1.f;
-        const float vs = a.cache.v_scale ? a.cache.v_scale[h] : 1.f;
-        float kx[4], vx[4];
-        for (uint64_t j = 0; j < n; ++j) {
-            const int32_t page = a.table[static_cast<uint64_t>(b) * a.max_pages + j / a.cache.page_size];
-            if (static_cast<uint32_t>(page) >= a.cache.num_pages) continue;
-            const uint64_t place = j % a.cache.page_size;
-            const uint64_t ka = page * a.cache.k_stride[0] + place * a.cache.k_stride[1] + h * a.cache.k_stride[2];
-            const uint64_t va = page * a.cache.v_stride[0] + place * a.cache.v_stride[1] + h * a.cache.v_stride[2];
-            for (uint32_t i = 0; i < 4; ++i) {
-                const uint32_t d = lane + 64 * i;
-                kx[i] = d < dim ? cached(a.cache.k, ka + d, a.cache.type) : 0.f;
-                vx[i] = d < dim ? cached(a.cache.v, va + d, a.cache.type) : 0.f;
-            }
-            visit(kx, vx, ks, vs);
-        }
-        int64_t j = self;
-        while (j >= 0) {
-            const uint64_t row = first + j;
-            int64_t up = j - 1;
-            if (a.parents) {
-                up = a.parents[row];
-                if (up < -1 || up >= j) break;
-            }
-            const uint16_t* const kr = static_cast<const uint16_t*>(a.k.data) + row * a.k.stride[0] + h * a.k.stride[1];
-            const uint16_t* const vr = static_cast<const uint16_t*>(a.v.data) + row * a.v.stride[0] + h * a.v.stride[1];
-            for (uint32_t i = 0; i < 4; ++i) {
-                const uint32_t d = lane + 64 * i;
-                kx[i] = d < dim ? coop_pages::to_float(kr[d], a.type) : 0.f;
-                vx[i] = d < dim ? coop_pages::to_float(vr[d], a.type) : 0.f;
-            }
-            visit(kx, vx, 1.f, 1.f);
-            j = up;
+    u32x4 q[kDim / 16];
+    {
+        const uint16_t* const base = static_cast<const uint16_t*>(a.q.data) +
+                                     (e.first + token) * a.q.stride[0] + qh * a.q.stride[1];
+#pragma unroll
+        for (uint32_t c = 0; c < kDim / 16; ++c) {
+            const uint32_t d = 16 * c + 8 * hi;
+            q[c] = u32x4{0, 0, 0, 0};
+            if (row_lives && d < dim) q[c] = *reinterpret_cast<const u32x4*>(base + d);
         }
     }
-    uint16_t* const to = a.out + (t * a.q_heads + hq) * dim;
-    for (uint32_t i = 0; i < 4; ++i)
-        if (lane + 64 * i < dim) to[lane + 64 * i] = from_float(is_void ? 0.f : o[i] / l, a.type);
+    f32x16 o[S::kDTiles];
+#pragma unroll
+    for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m = kLowest, l = 0.f;
+
+    const float new_scale = a.scale * kLog2e;
+    const float cached_scale = kE4M3 ? new_scale * a.cache.k_scale[item.head] : new_scale;
+    const float value_scale = kE4M3 ? a.cache.v_scale[item.head] : 1.f;
+    bool scaled = false;  // whether o has met the cached values' scale
+
+    // rows that do not count are read from a place that is there and left out
+    const uint8_t* const spare = static_cast<const uint8_t*>(a.q.data);
+    const uint64_t size = kE4M3 ? 1 : 2;
+    const uint8_t* const ck = static_cast<const uint8_t*>(a.cache.k) + item.head * a.cache.k_stride[2] * size;
+    const uint8_t* const cv = static_cast<const uint8_t*>(a.cache.v) + item.head * a.cache.v_stride[2] * size;
+
+    // A tile's page number for lane's key (lanes past the tile repeat it).
+    const uint32_t my_key = lane % kKeys;
+    auto page_of = [&](uint32_t tile) -> int32_t {
+        const uint32_t pos = tile * kKeys + my_key;
+        if (tile >= cached_tiles || pos >= e.cached) return -1;
+        return a.table[static_cast<uint64_t>(item.request) * a.max_pages + pos / page_size];
+    };
+    // Writes where the tile's rows are; returns which of its keys count.
+    auto locate = [&](uint32_t tile, int32_t page) -> uint64_t {
+        RowAt r = {spare, spare};
+        bool counts = false;
+        if (tile < cached_tiles) {
+            const uint32_t pos = tile * kKeys + my_key;
+            counts = pos < e.cached && static_cast<uint32_t>(page) < a.cache.num_pages;
+            if (counts) {
+                const uint64_t place = pos % page_size, p = static_cast<uint32_t>(page);
+                r.k = ck + (p * a.cache.k_stride[0] + place * a.cache.k_stride[1]) * size;
+                r.v = cv + (p * a.cache.v_stride[0] + place * a.cache.v_stride[1]) * size;
+            }
+        } else {
+            const uint32_t j = (cached_tiles + new_tiles - 1 - tile) * kKeys + my_key;
+            counts = j < e.tokens;
+            if (counts) {
+                r.k = reinterpret_cast<const uint8_t*>(static_cast<const uint16_t*>(a.k.data) +
+                                                       (e.first + j) * a.k.stride[0] + item.head * a.k.stride[1]);
+                r.v = reinterpret_cast<const uint8_t*>(static_cast<const uint16_t*>(a.v.data) +
+                                                       (e.first + j) * a.v.stride[0] + item.head * a.v.stride[1]);
+            }
+        }
+        if (lane < kKeys) rows_at[w][my_key] = r;
+        const uint64_t all = __ballot(counts);
+        return kKeys == 64 ? all : all & 0xffffffffu;
+    };
+    constexpr uint64_t kFull = kKeys == 64 ? ~0ull : 0xffffffffull;
+
+    u32x4 kreg[kLoads], vreg[kLoads];
+    const uint32_t chunk = gtid % S::kChunks, row_of_load = gtid / S::kChunks;
+    constexpr uint32_t kRowStep = S::kGroupThreads / S::kChunks;
+    constexpr uint32_t kChunks8 = S::kChunks / 2, kRowStep8 = S::kGroupThreads / kChunks8;
+    const uint32_t chunk8 = gtid % kChunks8, row_of_load8 = gtid / kChunks8;
+    auto load = [&](uint32_t tile) {
+        if (kE4M3 && tile < cached_tiles) {
+            const uint32_t byte = chunk8 * 16 < dim ? chunk8 * 16 : 0;
+#pragma unroll
+            for (uint32_t j = 0; j < kLoads8; ++j) {
+                const RowAt r = rows_at[w][row_of_load8 + j * kRowStep8];
+                kreg[j] = *reinterpret_cast<const u32x4*>(r.k + byte);
+                vreg[j] = *reinterpret_cast<const u32x4*>(r.v + byte);
+            }
+        } else {
+            const uint32_t byte = chunk * 8 < dim ? chunk * 16 : 0;
+#pragma unroll
+            for (uint32_t j = 0; j < kLoads; ++j) {
+                const RowAt r = rows_at[w][row_of_load + j * kRowStep];
+                kreg[j] = *reinterpret_cast<const u32x4*>(r.k + byte);
+                vreg[j] = *reinterpret_cast<const u32x4*>(r.v + byte);
+            }
+        }
+    };
+    auto put = [&](uint32_t r, uint32_t c, u32x4 kx, u32x4 vx) {
+        *reinterpret_cast<u32x4*>(key_tile + (r * S::kChunks + key_chunk<kDim>(r, c)) * 16) = kx;
+        *reinterpret_cast<u32x4*>(value_tile + (r * S::kChunks + value_chunk<kDim>(r, c)) * 16) = vx;
+    };
+    auto store = [&](uint32_t tile, uint64_t counts) {
+        const bool whole = counts == kFull && dim == kDim;
+        const u32x4 zero = {0, 0, 0, 0};
+        if (kE4M3 && tile < cached_tiles) {
+#pragma unroll
+            for (uint32_t j = 0; j < kLoads8; ++j) {
+                const uint32_t r = row_of_load8 + j * kRowStep8;
+                u32x4 kx = kreg[j], vx = vreg[j];
+                if (!whole && !(((counts >> r) & 1u) && chunk8 * 16 < dim)) kx = vx = zero;
+                u32x4 k2[2], v2[2];
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    k2[i >> 1][2 * (i & 1)] = T::template from_e4m3<false>(kx[i]);
+                    k2[i >> 1][2 * (i & 1) + 1] = T::template from_e4m3<true>(kx[i]);
+                    v2[i >> 1][2 * (i & 1)] = T::template from_e4m3<false>(vx[i]);
+                    v2[i >> 1][2 * (i & 1) + 1] = T::template from_e4m3<true>(vx[i]);
+                }
+                put(r, 2 * chunk8, k2[0], v2[0]);
+                put(r, 2 * chunk8 + 1, k2[1], v2[1]);
+            }
+        } else {
+            uint32_t found = 0;
+#pragma unroll
+            for (uint32_t j = 0; j < kLoads; ++j) {
+                const uint32_t r = row_of_load + j * kRowStep;
+                u32x4 kx = kreg[j], vx = vreg[j];
+                if (!whole && !(((counts >> r) & 1u) && chunk * 8 < dim)) kx = vx = zero;
+                put(r, chunk, kx, vx);
+                if (tile >= cached_tiles)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+                        found |= (vx[i] & T::kExponent) == T::kExponent ||
+                                 ((vx[i] >> 16) & T::kExponent) == T::kExponent;
+            }
+            if (tile >= cached_tiles) {
+                const bool any = __any(found);
+                if (lane == 0) odd[w] = any;
+            }
+        }
+    };
+    auto wave_sync = [&]() {  // a wavefront's LDS operations keep their order
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    auto sync = [&]() {
+        if (kRowWaves == 1) wave_sync();
+        else __syncthreads();
+    };
+
+    const uint32_t rounds = last > first ? ceil_div(last - first, S::kGroups) : 0;
+    uint32_t tile = first + group;
+    uint64_t counts = 0, next_counts = 0;
+    int32_t next_page = -1;
+    if (rounds) {
+        const int32_t page = tile < last ? page_of(tile) : -1;
+        next_page = tile + S::kGroups < last ? page_of(tile + S::kGroups) : -1;
+        if (tile < last) counts = locate(tile, page);
+        sync();
+        if (tile < last) load(tile);
+        sync();
+    }
+    for (uint32_t round = 0; round < rounds; ++round, tile += S::kGroups) {
+        const bool here = tile < last, more = tile + S::kGroups < last;
+        if (here) store(tile, counts);
+        if (more) next_counts = locate(tile + S::kGroups, next_page);
+        sync();
+        if (tile + 2 * S::kGroups < last) next_page = page_of(tile + 2 * S::kGroups);
+        if (more) load(tile + S::kGroups);
+        if (here) {
+            const bool is_new = tile >= cached_tiles;
+            f32x16 s[S::kSTiles];
+#pragma unroll
+            for (uint32_t t = 0; t < S::kSTiles; ++t) {
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) s[t][i] = 0.f;
+                const uint32_t r = 32 * t + n;
+#pragma unroll
+                for (uint32_t c = 0; c < kDim / 16; ++c) {
+                    const u32x4 kx = *reinterpret_cast<const u32x4*>(
+                        key_tile + (r * S::kChunks + key_chunk<kDim>(r, 2 * c + hi)) * 16);
+                    s[t] = T::mfma(kx, q[c], s[t]);
+                }
+            }
+            // which keys this lane's row sees
+            uint64_t sees = counts;
+            if (is_new) {
+                const int32_t k0 = static_cast<int32_t>((cached_tiles + new_tiles - 1 - tile) * kKeys);
+                sees = 0;
+                if (!parents) {
+                    const int32_t past = static_cast<int32_t>(token) - k0;
+                    if (row_lives && past >= 0) sees = past >= 63 ? ~0ull : (2ull << past) - 1;
+                    sees &= kFull;
+                } else {
+                    while (at >= k0 + static_cast<int32_t>(kKeys)) climb();
+                    while (at >= k0) {
+                        sees |= 1ull << (at - k0);
+                        climb();
+                    }
+                }
+            }
+            const float factor = is_new ? new_scale : cached_scale;
+            const bool masked = !__all(sees == kFull);
+            float top = kLowest;
+#pragma unroll
+            for (uint32_t t = 0; t < S::kSTiles; ++t) {
+                const uint32_t bits = static_cast<uint32_t>(sees >> (32 * t)) >> (4 * hi);
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) {
+                    float x = s[t][i] * factor;
+                    if (masked && !((bits >> (8 * (i >> 2) + (i & 3))) & 1u)) x = kLowest;
+                    s[t][i] = x;
+                    top = fmaxf(top, x);
+                }
+            }
+            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            const float m2 = fmaxf(m, top);
+            const float base = m2 == kLowest ? 0.f : m2;  // no score above the lowest yet
+            const float shrink = __builtin_amdgcn_exp2f(m - base);
+            m = m2;
+            float sum = 0.f;
+            uint32_t p[S::kSTiles][8];
+#pragma unroll
+            for (uint32_t t = 0; t < S::kSTiles; ++t)
+#pragma unroll
+                for (uint32_t i = 0; i < 16; i += 2) {
+                    const float x = __builtin_amdgcn_exp2f(s[t][i] - base);
+                    const float y = __builtin_amdgcn_exp2f(s[t][i + 1] - base);
+                    sum += x + y;
+                    p[t][i / 2] = T::pack(x, y);
+                }
+            l = l * shrink + sum;
+            float grow = shrink;
+            if (kE4M3 && is_new && !scaled) {
+                grow *= value_scale;
+                scaled = true;
+            }
+            if (!__all(grow == 1.f))
+#pragma unroll
+                for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+                    for (uint32_t i = 0; i < 16; ++i) o[t][i] *= grow;
+            bool plain = true;
+            if (is_new) {
+                uint32_t any = 0;
+                for (uint32_t i = 0; i < kRowWaves; ++i) any |= odd[group * kRowWaves + i];
+                plain = !__any(any);
+            }
+            if (plain) {
+                const uint32_t g = lane & 15u;
+#pragma unroll
+                for (uint32_t t = 0; t < S::kSTiles; ++t)
+#pragma unroll
+                    for (uint32_t half = 0; half < 2; ++half) {
+                        const u32x4 px = {p[t][4 * half], p[t][4 * half + 1], p[t][4 * half + 2],
+                                          p[t][4 * half + 3]};
+                        const uint32_t r = 32 * t + 16 * half + 4 * hi + (g >> 2);
+#pragma unroll
+                        for (uint32_t dt = 0; dt < S::kDTiles; ++dt) {
+                            const uint32_t d = 32 * dt + (lane & 16u) + 4 * (g & 3u);
+                            typedef __attribute__((address_space(3))) s16x4 Lds;
+                            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
+                                value_tile + (r * S::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2));
+                            const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
+                                value_tile + ((r + 8) * S::kChunks + value_chunk<kDim>(r + 8, d / 8)) * 16 +
+                                (d & 4) * 2));
+                            const uint2 a0 = __builtin_bit_cast(uint2, v0), a1 = __builtin_bit_cast(uint2, v1);
+                            const u32x4 vx = {a0.x, a0.y, a1.x, a1.y};
+                            o[dt] = T::mfma(vx, px, o[dt]);
+                        }
+                    }
+            } else {
+                // Some value of these new tokens is not finite: zero weights do
+                // not keep it from rows that do not see it, so each row adds
+                // the keys that it sees one by one.
+#pragma unroll
+                for (uint32_t t = 0; t < S::kSTiles; ++t) {
+                    wave_sync();
+#pragma unroll
+                    for (uint32_t i = 0; i < 16; ++i)
+                        weights[w][8 * (i >> 2) + 4 * hi + (i & 3)][n] =
+                            static_cast<uint16_t>(p[t][i / 2] >> (16 * (i & 1)));
+                    wave_sync();
+                    const uint32_t bits = static_cast<uint32_t>(sees >> (32 * t));
+                    for (uint32_t key = 0; key < 32; ++key) {
+                        const float x = T::value(weights[w][key][n]);
+                        const bool use = (bits >> key) & 1u;
+                        const uint32_t r = 32 * t + key;
+#pragma unroll
+                        for (uint32_t dt = 0; dt < S::kDTiles; ++dt)
+#pragma unroll
+                            for (uint32_t i = 0; i < 16; i += 4) {
+                                const uint32_t d = 32 * dt + 2 * i + 4 * hi;
+                                const uint2 four = *reinterpret_cast<const uint2*>(
+                                    value_tile + (r * S::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2);
+                                const uint16_t v4[4] = {
+                                    static_cast<uint16_t>(four.x), static_cast<uint16_t>(four.x >> 16),
+                                    static_cast<uint16_t>(four.y), static_cast<uint16_t>(four.y >> 16)};
+#pragma unroll
+                                for (uint32_t u = 0; u < 4; ++u)
+                                    o[dt][i + u] += use ? x * T::value(v4[u]) : 0.f;
+                            }
+                    }
+                }
+            }
+        }
+        counts = next_counts;
+        sync();
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (kE4M3 && !scaled)
+#pragma unroll
+        for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) o[t][i] *= value_scale;
+
+    const bool is_whole = item.part == kWhole;
+    bool is_void = false;
+    if (parents && row_lives) {
+        const int32_t p = parents[token];
+        is_void = p < -1 || p >= static_cast<int32_t>(token);
+    }
+    if constexpr (S::kGroups > 1) {
+        // join the groups: each scales its part to the common maximum and adds
+        // it to the first one's, a group after the other
+        __syncthreads();
+        if (hi == 0) {
+            joined[w][n][0] = m;
+            joined[w][n][1] = l;
+        }
+        __syncthreads();
+        float m_all = kLowest, l_all = 0.f;
+        for (uint32_t g = 0; g < S::kGroups; ++g) m_all = fmaxf(m_all, joined[g * kRowWaves + row_wave][n][0]);
+        const float base = m_all == kLowest ? 0.f : m_all;
+        for (uint32_t g = 0; g < S::kGroups; ++g)
+            l_all += joined[g * kRowWaves + row_wave][n][1] *
+                     __builtin_amdgcn_exp2f(joined[g * kRowWaves + row_wave][n][0] - base);
+        const float part = __builtin_amdgcn_exp2f(m - base);
+        // [row wave][element][lane]: every lane has the same elements in each group
+        float* const sums = reinterpret_cast<float*>(tiles) + row_wave * (kDim / 2) * 64 + lane;
+        static_assert(kRowWaves * kDim * 32 * 4 <= S::kBytes, "the sums fit where the tiles were");
+        for (uint32_t g = 1; g < S::kGroups; ++g) {
+            if (group == g)
+#pragma unroll
+                for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+                    for (uint32_t i = 0; i < 16; ++i) {
+                        float* const x = sums + (16 * t + i) * 64;
+                        *x = (g == 1 ? 0.f : *x) + o[t][i] * part;
+                    }
+            __syncthreads();
+        }
+        if (group != 0) return;
+#pragma unroll
+        for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) o[t][i] = o[t][i] * part + sums[(16 * t + i) * 64];
+        m = m_all;
+        l = l_all;
+    }
+    if (!row_lives) return;
+    if (is_whole) {
+        uint16_t* const to = a.out + ((e.first + token) * a.q_heads + qh) * dim;
+#pragma unroll
+        for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; i += 4) {
+                const uint32_t d = 32 * t + 2 * i + 4 * hi;
+                if (d >= dim) continue;
+                uint2 x = make_uint2(T::pack(o[t][i] / l, o[t][i + 1] / l),
+                                     T::pack(o[t][i + 2] / l, o[t][i + 3] / l));
+                if (is_void) x = make_uint2(0, 0);
+                *reinterpret_cast<uint2*>(to + d) = x;
+            }
+    } else {
+        const uint64_t at_row = static_cast<uint64_t>(item.part) * a.part_rows + row_wave * kRows + n;
+        float* const to = a.part_out + at_row * kDim;
+#pragma unroll
+        for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4*>(to + 32 * t + 2 * i + 4 * hi) =
+                    make_float4(o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]);
+        if (hi == 0) a.part_sum[at_row] = make_float2(m, l);
+    }
 }
+
+// Joins the parts of rows whose keys were cut: one wavefront a row.
+template <class T, uint32_t kDim>
+__global__ __launch_bounds__(kThreads) void attention_join_kernel(Args a) {
+    constexpr uint32_t kEach = kDim / 64;
+    const uint32_t lane = threadIdx.x & 63u;
+    const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint64_t all = static_cast<uint64_t>(a.head->joins) * a.part_rows;
+    for (uint64_t i = blockIdx.x * 4ull + w; i < all; i += gridDim.x * 4ull) {
+        const Join j = a.joins[i / a.part_rows];
+        const uint32_t r = static_cast<uint32_t>(i % a.part_rows);
+        const Extent e = extent(a, j.request);
+        const uint32_t row = j.row_tile * a.row_tile_rows + r;
+        if (row >= e.tokens * a.group) continue;
+        const uint32_t token = row / a.group, qh = j.head * a.group + row % a.group;
+        const uint64_t first = static_cast<uint64_t>(j.first) * a.part_rows + r;
+        float m = kLowest;
+        for (uint32_t p = lane; p < j.parts; p += 64)
+            m = fmaxf(m, a.part_sum[first + static_cast<uint64_t>(p) * a.part_rows].x);
+        for (uint32_t d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+        const float base = m == kLowest ? 0.f : m;
+        float l = 0.f, o[kEach];
+        for (uint32_t c = 0; c < kEach; ++c) o[c] = 0.f;
+        for (uint32_t p = 0; p < j.parts; ++p) {
+            const uint64_t at = first + static_cast<uint64_t>(p) * a.part_rows;
+            const float2 ml = a.part_sum[at];
+            const float x = __builtin_amdgcn_exp2f(ml.x - base);
+            l += ml.y * x;
+            for (uint32_t c = 0; c < kEach; ++c) o[c] += a.part_out[at * kDim + lane * kEach + c] * x;
+        }
+        bool is_void = false;
+        if (a.parents) {
+            const int32_t p = a.parents[e.first + token];
+            is_void = p < -1 || p >= static_cast<int32_t>(token);
+        }
+        const uint32_t dim = static_cast<uint32_t>(a.cache.dim);
+        uint16_t* const to = a.out + ((e.first + token) * a.q_heads + qh) * dim;
+        for (uint32_t c = 0; c < kEach; ++c)
+            if (lane * kEach + c < dim)
+                to[lane * kEach + c] =
+                    static_cast<uint16_t>(is_void ? 0u : T::pack(o[c] / l, 0.f) & 0xffffu);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
 
 constexpr uint64_t kMost = (1ull << 31) - 1;
 
@@ -123,7 +813,57 @@ bool counts_valid(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t
                   uint64_t dim) {
     return heads && heads <= coop_pages::kMaxHeads && q_heads && q_heads <= coop_pages::kMaxHeads &&
            q_heads % heads == 0 && requests < kMost && tokens <= kMost &&
-           tokens * q_heads <= kMost && dim && dim <= coop_pages::kMaxDim && dim % 8 == 0;
+           tokens * q_heads <= kMost && requests * heads <= kMost && dim &&
+           dim <= coop_pages::kMaxDim && dim % 8 == 0;
+}
+
+struct Plan {
+    uint32_t dim;        // padded
+    uint32_t row_waves;
+    uint32_t tile_keys;
+    uint32_t target;
+    uint32_t part_rows;
+    uint64_t max_items, pairs;
+    size_t items_offset, joins_offset, sum_offset, out_offset, bytes;
+};
+
+Plan plan_of(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t heads, uint64_t dim) {
+    Plan p;
+    p.dim = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
+    const uint64_t group = q_heads / heads, rows = tokens * group;
+    // wavefronts along the rows: as many as an average request fills
+    const uint64_t mean = requests ? (rows + requests - 1) / requests : 0;
+    p.row_waves = mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
+    p.tile_keys = p.row_waves == 1 ? 32 : 64;
+    p.target = 1024;
+    const uint64_t tile_rows = kRows * p.row_waves;
+    p.part_rows = static_cast<uint32_t>(rows < tile_rows ? rows : tile_rows);
+    p.pairs = heads * ((rows + tile_rows - 1) / tile_rows + requests);
+    p.max_items = 2ull * p.target + p.pairs;
+    auto next = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
+    p.items_offset = 256;
+    p.joins_offset = next(p.items_offset + p.max_items * sizeof(Item));
+    p.sum_offset = next(p.joins_offset + p.target * sizeof(Join));
+    p.out_offset = next(p.sum_offset + 2ull * p.target * p.part_rows * sizeof(float2));
+    p.bytes = p.out_offset + 2ull * p.target * p.part_rows * p.dim * sizeof(float);
+    return p;
+}
+
+template <class T, bool kE4M3, uint32_t kDim>
+void launch(const Plan& p, const Args& a, uint32_t joins, hipStream_t s) {
+    auto kernel = p.row_waves == 1   ? tree_attention_kernel<T, kE4M3, kDim, 1>
+                  : p.row_waves == 2 ? tree_attention_kernel<T, kE4M3, kDim, 2>
+                                     : tree_attention_kernel<T, kE4M3, kDim, 4>;
+    hipLaunchKernelGGL(kernel, dim3(a.max_items), dim3(kThreads), 0, s, a);
+    if (joins)
+        hipLaunchKernelGGL((attention_join_kernel<T, kDim>), dim3(joins), dim3(kThreads), 0, s, a);
+}
+
+template <class T, bool kE4M3>
+void launch_dim(const Plan& p, const Args& a, uint32_t joins, hipStream_t s) {
+    if (p.dim == 64) launch<T, kE4M3, 64>(p, a, joins, s);
+    else if (p.dim == 128) launch<T, kE4M3, 128>(p, a, joins, s);
+    else launch<T, kE4M3, 256>(p, a, joins, s);
 }
 
 }  // namespace
@@ -135,7 +875,8 @@ coop_status_t coop_tree_attention_workspace_size(uint64_t num_requests, uint64_t
                                                  size_t* bytes_out) {
     if (!bytes_out || !counts_valid(num_requests, num_tokens, q_heads, heads, dim))
         return COOP_ERR_INVALID;
-    *bytes_out = 0;
+    *bytes_out =
+        num_requests && num_tokens ? plan_of(num_requests, num_tokens, q_heads, heads, dim).bytes : 0;
     return COOP_OK;
 }
 
@@ -150,7 +891,7 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     if (!q || !k_new || !v_new || !cache) return COOP_ERR_INVALID;
     if (const coop_status_t rc = coop_pages::check_cache(*cache, type)) return rc;
     if (!counts_valid(num_requests, num_tokens, q_heads, cache->heads, cache->dim) ||
-        max_pages > kMost)
+        max_pages > kMost || max_pages * cache->page_size > kMost)
         return COOP_ERR_INVALID;
     if (num_tokens == 0) return COOP_OK;
     if (!coop_pages::rows_valid(*q, num_tokens) || !coop_pages::rows_valid(*k_new, num_tokens) ||
@@ -159,10 +900,8 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     if (!out || !coop_pages::aligned16(out) || !token_offsets) return COOP_ERR_INVALID;
     if (num_requests == 0) return COOP_OK;
     if (!lengths || (max_pages && !table)) return COOP_ERR_INVALID;
-    size_t need = 0;
-    coop_tree_attention_workspace_size(num_requests, num_tokens, q_heads, cache->heads, cache->dim,
-                                       &need);
-    if (need && (!workspace || workspace_bytes < need)) return COOP_ERR_WORKSPACE;
+    const Plan p = plan_of(num_requests, num_tokens, q_heads, cache->heads, cache->dim);
+    if (!workspace || workspace_bytes < p.bytes) return COOP_ERR_WORKSPACE;
     Args a;
     a.q = *q;
     a.k = *k_new;
@@ -177,10 +916,39 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     a.requests = static_cast<uint32_t>(num_requests);
     a.max_pages = static_cast<uint32_t>(max_pages);
     a.q_heads = static_cast<uint32_t>(q_heads);
-    a.type = static_cast<uint32_t>(type);
+    a.group = static_cast<uint32_t>(q_heads / cache->heads);
     a.scale = scale;
-    hipLaunchKernelGGL(tree_attention_kernel, dim3(static_cast<uint32_t>(num_tokens * q_heads)),
-                       dim3(64), 0, static_cast<hipStream_t>(stream), a);
+    a.tile_keys = p.tile_keys;
+    a.row_tile_rows = kRows * p.row_waves;
+    a.least = 512 / p.tile_keys;
+    a.chunk_multiple = 4 / p.row_waves;
+    a.part_rows = p.part_rows;
+    // the tiles that there can be at most
+    const uint64_t tiles = (max_pages * cache->page_size + p.tile_keys - 1) / p.tile_keys +
+                           (num_tokens + p.tile_keys - 1) / p.tile_keys;
+    const unsigned __int128 most = static_cast<unsigned __int128>(p.pairs) * tiles / a.least + 1;
+    a.target = most < p.target ? static_cast<uint32_t>(most) : p.target;
+    a.max_items = static_cast<uint32_t>(2ull * a.target + p.pairs);
+    char* const ws = static_cast<char*>(workspace);
+    a.head = reinterpret_cast<Head*>(ws);
+    a.items = reinterpret_cast<Item*>(ws + p.items_offset);
+    a.joins = reinterpret_cast<Join*>(ws + p.joins_offset);
+    a.part_sum = reinterpret_cast<float2*>(ws + p.sum_offset);
+    a.part_out = reinterpret_cast<float*>(ws + p.out_offset);
+    // rows can be cut only if one can have more tiles than the shortest range
+    const uint64_t join_rows = static_cast<uint64_t>(a.target) * a.part_rows;
+    const uint32_t joins = tiles > a.least ? static_cast<uint32_t>(join_rows / 4 < 2048 ? join_rows / 4 + 1 : 2048) : 0;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipLaunchKernelGGL(attention_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return COOP_ERR_HIP;
+    const bool e4m3 = cache->type == COOP_E4M3;
+    if (type == COOP_BF16) {
+        if (e4m3) launch_dim<Bf16, true>(p, a, joins, s);
+        else launch_dim<Bf16, false>(p, a, joins, s);
+    } else {
+        if (e4m3) launch_dim<Fp16, true>(p, a, joins, s);
+        else launch_dim<Fp16, false>(p, a, joins, s);
+    }
     return hipGetLastError() == hipSuccess ? COOP_OK : COOP_ERR_HIP;
 }
 
