@@ -290,7 +290,7 @@ struct Fp16 {
 template <class T, bool kE4M3, uint32_t kDim, uint32_t kRowWaves>
 struct Shape {
     static constexpr uint32_t kGroups = 4 / kRowWaves;
-    static constexpr uint32_t kKeys = kRowWaves == 1 ? 32 : 64;  // of a tile
+    static constexpr uint32_t kKeys = kRowWaves == 4 ? 64 : 32;  // of a tile
     static constexpr uint32_t kGroupThreads = 64 * kRowWaves;
     static constexpr uint32_t kChunks = kDim / 8;  // 16-byte chunks of a row in LDS
     static constexpr uint32_t kLoads = kKeys * kChunks / kGroupThreads;      // a thread's, a tile
@@ -322,10 +322,10 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     using S = Shape<T, kE4M3, kDim, kRowWaves>;
     constexpr uint32_t kKeys = S::kKeys, kLoads = S::kLoads, kLoads8 = S::kLoads8;
     __shared__ __align__(16) uint8_t tiles[S::kBytes];
+    __shared__ __align__(16) uint8_t queries[kRowWaves * kRows * kDim * 2];
     __shared__ RowAt rows_at[4][kKeys];           // one copy a wavefront
     __shared__ int32_t tree[kParentsInLds];
-    __shared__ uint16_t weights[4][32][kRows];    // only for values that are not finite
-    __shared__ uint32_t odd[4];                   // whether a wavefront stored such values
+    __shared__ uint32_t odd;                      // whether new values are not all finite
     __shared__ float joined[4][kRows][2];
 
     if (blockIdx.x >= a.head->items) return;
@@ -357,40 +357,45 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     const bool in_lds = a.parents && e.tokens <= kParentsInLds && last > cached_tiles;
     if (in_lds)
         for (uint32_t i = tid; i < e.tokens; i += kThreads) tree[i] = a.parents[e.first + i];
+    if (tid == 0) odd = 0;
     __syncthreads();
     const int32_t* const parents = a.parents ? a.parents + e.first : nullptr;
     auto parent_of = [&](int32_t i) { return in_lds ? tree[i] : parents[i]; };
 
-    // the row's place on its way up: a token that it sees, and that one's parent
+    // the row's place on its way up: a token that it sees (-1: none is left),
+    // and that one's parent
     int32_t at = -1, up = -1;
-    if (row_lives && last > cached_tiles) {
-        at = static_cast<int32_t>(token);
+    auto start = [&]() {
+        at = row_lives && last > cached_tiles ? static_cast<int32_t>(token) : -1;
         up = at - 1;
-        if (parents) {
+        if (at >= 0 && parents) {
             up = parent_of(at);
             if (up < -1 || up >= at) at = -1;
         }
-    }
+    };
     auto climb = [&]() {
         const int32_t next = up;
         if (next < 0) {
             at = -1;
             return;
         }
-        const int32_t above = parent_of(next);
+        const int32_t above = parents ? parent_of(next) : next - 1;
         at = above < -1 || above >= next ? -1 : next;
         up = above;
     };
+    start();
 
-    u32x4 q[kDim / 16];
-    {
+    // the rows' queries, permuted as the keys are
+    uint8_t* const query_tile = queries + row_wave * kRows * kDim * 2;
+    if (group == 0) {
         const uint16_t* const base = static_cast<const uint16_t*>(a.q.data) +
                                      (e.first + token) * a.q.stride[0] + qh * a.q.stride[1];
 #pragma unroll
         for (uint32_t c = 0; c < kDim / 16; ++c) {
             const uint32_t d = 16 * c + 8 * hi;
-            q[c] = u32x4{0, 0, 0, 0};
-            if (row_lives && d < dim) q[c] = *reinterpret_cast<const u32x4*>(base + d);
+            u32x4 x = {0, 0, 0, 0};
+            if (row_lives && d < dim) x = *reinterpret_cast<const u32x4*>(base + d);
+            *reinterpret_cast<u32x4*>(query_tile + (n * S::kChunks + key_chunk<kDim>(n, 2 * c + hi)) * 16) = x;
         }
     }
     f32x16 o[S::kDTiles];
@@ -501,17 +506,18 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
                 const uint32_t r = row_of_load + j * kRowStep;
                 u32x4 kx = kreg[j], vx = vreg[j];
                 if (!whole && !(((counts >> r) & 1u) && chunk * 8 < dim)) kx = vx = zero;
-                put(r, chunk, kx, vx);
                 if (tile >= cached_tiles)
 #pragma unroll
                     for (uint32_t i = 0; i < 4; ++i)
-                        found |= (vx[i] & T::kExponent) == T::kExponent ||
-                                 ((vx[i] >> 16) & T::kExponent) == T::kExponent;
+#pragma unroll
+                        for (uint32_t half = 0; half < 32; half += 16)
+                            if (((vx[i] >> half) & T::kExponent) == T::kExponent) {
+                                found = 1;
+                                vx[i] &= 0xffff0000u >> half;
+                            }
+                put(r, chunk, kx, vx);
             }
-            if (tile >= cached_tiles) {
-                const bool any = __any(found);
-                if (lane == 0) odd[w] = any;
-            }
+            if (found) odd = 1;
         }
     };
     auto wave_sync = [&]() {  // a wavefront's LDS operations keep their order
@@ -546,15 +552,18 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
             const bool is_new = tile >= cached_tiles;
             f32x16 s[S::kSTiles];
 #pragma unroll
-            for (uint32_t t = 0; t < S::kSTiles; ++t) {
+            for (uint32_t t = 0; t < S::kSTiles; ++t)
 #pragma unroll
                 for (uint32_t i = 0; i < 16; ++i) s[t][i] = 0.f;
-                const uint32_t r = 32 * t + n;
 #pragma unroll
-                for (uint32_t c = 0; c < kDim / 16; ++c) {
-                    const u32x4 kx = *reinterpret_cast<const u32x4*>(
-                        key_tile + (r * S::kChunks + key_chunk<kDim>(r, 2 * c + hi)) * 16);
-                    s[t] = T::mfma(kx, q[c], s[t]);
+            for (uint32_t c = 0; c < kDim / 16; ++c) {
+                const uint32_t place = (n * S::kChunks + key_chunk<kDim>(n, 2 * c + hi)) * 16;
+                const u32x4 qx = *reinterpret_cast<const u32x4*>(query_tile + place);
+#pragma unroll
+                for (uint32_t t = 0; t < S::kSTiles; ++t) {
+                    // (rows 32 apart are permuted alike)
+                    const u32x4 kx = *reinterpret_cast<const u32x4*>(key_tile + place + t * 32 * kDim * 2);
+                    s[t] = T::mfma(kx, qx, s[t]);
                 }
             }
             // which keys this lane's row sees
@@ -615,69 +624,28 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
                 for (uint32_t t = 0; t < S::kDTiles; ++t)
 #pragma unroll
                     for (uint32_t i = 0; i < 16; ++i) o[t][i] *= grow;
-            bool plain = true;
-            if (is_new) {
-                uint32_t any = 0;
-                for (uint32_t i = 0; i < kRowWaves; ++i) any |= odd[group * kRowWaves + i];
-                plain = !__any(any);
-            }
-            if (plain) {
-                const uint32_t g = lane & 15u;
+            const uint32_t g = lane & 15u;
 #pragma unroll
-                for (uint32_t t = 0; t < S::kSTiles; ++t)
+            for (uint32_t t = 0; t < S::kSTiles; ++t)
 #pragma unroll
-                    for (uint32_t half = 0; half < 2; ++half) {
-                        const u32x4 px = {p[t][4 * half], p[t][4 * half + 1], p[t][4 * half + 2],
-                                          p[t][4 * half + 3]};
-                        const uint32_t r = 32 * t + 16 * half + 4 * hi + (g >> 2);
+                for (uint32_t half = 0; half < 2; ++half) {
+                    const u32x4 px = {p[t][4 * half], p[t][4 * half + 1], p[t][4 * half + 2],
+                                      p[t][4 * half + 3]};
+                    const uint32_t r = 32 * t + 16 * half + 4 * hi + (g >> 2);
 #pragma unroll
-                        for (uint32_t dt = 0; dt < S::kDTiles; ++dt) {
-                            const uint32_t d = 32 * dt + (lane & 16u) + 4 * (g & 3u);
-                            typedef __attribute__((address_space(3))) s16x4 Lds;
-                            const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
-                                value_tile + (r * S::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2));
-                            const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
-                                value_tile + ((r + 8) * S::kChunks + value_chunk<kDim>(r + 8, d / 8)) * 16 +
-                                (d & 4) * 2));
-                            const uint2 a0 = __builtin_bit_cast(uint2, v0), a1 = __builtin_bit_cast(uint2, v1);
-                            const u32x4 vx = {a0.x, a0.y, a1.x, a1.y};
-                            o[dt] = T::mfma(vx, px, o[dt]);
-                        }
-                    }
-            } else {
-                // Some value of these new tokens is not finite: zero weights do
-                // not keep it from rows that do not see it, so each row adds
-                // the keys that it sees one by one.
-#pragma unroll
-                for (uint32_t t = 0; t < S::kSTiles; ++t) {
-                    wave_sync();
-#pragma unroll
-                    for (uint32_t i = 0; i < 16; ++i)
-                        weights[w][8 * (i >> 2) + 4 * hi + (i & 3)][n] =
-                            static_cast<uint16_t>(p[t][i / 2] >> (16 * (i & 1)));
-                    wave_sync();
-                    const uint32_t bits = static_cast<uint32_t>(sees >> (32 * t));
-                    for (uint32_t key = 0; key < 32; ++key) {
-                        const float x = T::value(weights[w][key][n]);
-                        const bool use = (bits >> key) & 1u;
-                        const uint32_t r = 32 * t + key;
-#pragma unroll
-                        for (uint32_t dt = 0; dt < S::kDTiles; ++dt)
-#pragma unroll
-                            for (uint32_t i = 0; i < 16; i += 4) {
-                                const uint32_t d = 32 * dt + 2 * i + 4 * hi;
-                                const uint2 four = *reinterpret_cast<const uint2*>(
-                                    value_tile + (r * S::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2);
-                                const uint16_t v4[4] = {
-                                    static_cast<uint16_t>(four.x), static_cast<uint16_t>(four.x >> 16),
-                                    static_cast<uint16_t>(four.y), static_cast<uint16_t>(four.y >> 16)};
-#pragma unroll
-                                for (uint32_t u = 0; u < 4; ++u)
-                                    o[dt][i + u] += use ? x * T::value(v4[u]) : 0.f;
-                            }
+                    for (uint32_t dt = 0; dt < S::kDTiles; ++dt) {
+                        const uint32_t d = 32 * dt + (lane & 16u) + 4 * (g & 3u);
+                        typedef __attribute__((address_space(3))) s16x4 Lds;
+                        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
+                            value_tile + (r * S::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2));
+                        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
+                            value_tile + ((r + 8) * S::kChunks + value_chunk<kDim>(r + 8, d / 8)) * 16 +
+                            (d & 4) * 2));
+                        const uint2 a0 = __builtin_bit_cast(uint2, v0), a1 = __builtin_bit_cast(uint2, v1);
+                        const u32x4 vx = {a0.x, a0.y, a1.x, a1.y};
+                        o[dt] = T::mfma(vx, px, o[dt]);
                     }
                 }
-            }
         }
         counts = next_counts;
         sync();
@@ -734,6 +702,26 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
         l = l_all;
     }
     if (!row_lives) return;
+    if (last > cached_tiles && odd) {
+        // Values that are not finite were left out above, where a weight of
+        // zero would not keep them from rows that do not see them.  The rows
+        // that see them take them here (weights are above zero).
+        const int32_t below = static_cast<int32_t>((cached_tiles + new_tiles - max(first, cached_tiles)) * kKeys);
+        const int32_t from = static_cast<int32_t>((cached_tiles + new_tiles - last) * kKeys);
+        for (start(); at >= from; climb()) {
+            if (at >= below) continue;
+            const uint16_t* const v = static_cast<const uint16_t*>(a.v.data) +
+                                      (e.first + at) * a.v.stride[0] + item.head * a.v.stride[1];
+#pragma unroll
+            for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) {
+                    const uint32_t d = 32 * t + 8 * (i >> 2) + 4 * hi + (i & 3);
+                    const uint16_t bits = d < dim ? v[d] : 0;
+                    if ((bits & T::kExponent) == T::kExponent) o[t][i] += T::value(bits);
+                }
+        }
+    }
     if (is_whole) {
         uint16_t* const to = a.out + ((e.first + token) * a.q_heads + qh) * dim;
 #pragma unroll
@@ -834,7 +822,7 @@ Plan plan_of(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t head
     // wavefronts along the rows: as many as an average request fills
     const uint64_t mean = requests ? (rows + requests - 1) / requests : 0;
     p.row_waves = mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
-    p.tile_keys = p.row_waves == 1 ? 32 : 64;
+    p.tile_keys = p.row_waves == 4 ? 64 : 32;
     p.target = 1024;
     const uint64_t tile_rows = kRows * p.row_waves;
     p.part_rows = static_cast<uint32_t>(rows < tile_rows ? rows : tile_rows);
