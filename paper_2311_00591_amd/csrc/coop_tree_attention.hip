@@ -51,6 +51,7 @@ constexpr uint32_t kParentsInLds = 512;   // trees up to this size are walked in
 constexpr uint32_t kPlanThreads = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -__builtin_inff();
+constexpr float kSlack = 8.f;  // how far, in powers of two, scores may pass the sums' base
 
 struct Item {  // rows [32 kRowWaves rt, ...) of a request and head, tiles [first, last)
     uint32_t request, row_tile, head, first, last;
@@ -79,6 +80,7 @@ struct Args {
     uint16_t* out;
     uint64_t tokens;
     uint32_t requests, max_pages, q_heads, group;
+    uint32_t page_shift;  // page_size is 2^page_shift; 32: not a power of two
     float scale;
     // the plan and the workspace
     uint32_t tile_keys, row_tile_rows, target, least, chunk_multiple, max_items, part_rows;
@@ -337,6 +339,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     const uint32_t n = lane & 31u, hi = lane >> 5;
     const uint32_t dim = static_cast<uint32_t>(a.cache.dim);
     const uint32_t page_size = static_cast<uint32_t>(a.cache.page_size);
+    const bool alike = a.cache.k_stride[0] == a.cache.v_stride[0] && a.cache.k_stride[1] == a.cache.v_stride[1];
+    auto page_at = [&](uint32_t pos) { return a.page_shift < 32 ? pos >> a.page_shift : pos / page_size; };
     const Extent e = extent(a, item.request);
     const uint32_t rows = e.tokens * a.group;
     const uint32_t row0 = item.row_tile * (kRows * kRowWaves);
@@ -421,7 +425,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     auto page_of = [&](uint32_t tile) -> int32_t {
         const uint32_t pos = tile * kKeys + my_key;
         if (tile >= cached_tiles || pos >= e.cached) return -1;
-        return a.table[static_cast<uint64_t>(item.request) * a.max_pages + pos / page_size];
+        return a.table[static_cast<uint64_t>(item.request) * a.max_pages + page_at(pos)];
     };
     // Writes where the tile's rows are; returns which of its keys count.
     auto locate = [&](uint32_t tile, int32_t page) -> uint64_t {
@@ -431,9 +435,10 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
             const uint32_t pos = tile * kKeys + my_key;
             counts = pos < e.cached && static_cast<uint32_t>(page) < a.cache.num_pages;
             if (counts) {
-                const uint64_t place = pos % page_size, p = static_cast<uint32_t>(page);
-                r.k = ck + (p * a.cache.k_stride[0] + place * a.cache.k_stride[1]) * size;
-                r.v = cv + (p * a.cache.v_stride[0] + place * a.cache.v_stride[1]) * size;
+                const uint64_t place = pos - page_at(pos) * page_size, p = static_cast<uint32_t>(page);
+                const uint64_t at_k = (p * a.cache.k_stride[0] + place * a.cache.k_stride[1]) * size;
+                r.k = ck + at_k;
+                r.v = cv + (alike ? at_k : (p * a.cache.v_stride[0] + place * a.cache.v_stride[1]) * size);
             }
         } else {
             const uint32_t j = (cached_tiles + new_tiles - 1 - tile) * kKeys + my_key;
@@ -583,38 +588,49 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
                     }
                 }
             }
-            const float factor = is_new ? new_scale : cached_scale;
-            const bool masked = !__all(sees == kFull);
-            float top = kLowest;
+            // scores are s * factor; where keys are masked, or the factor is
+            // negative and does not keep the maximum, they are formed first
+            float factor = is_new ? new_scale : cached_scale;
+            if (factor < 0.f || !__all(sees == kFull)) {
 #pragma unroll
-            for (uint32_t t = 0; t < S::kSTiles; ++t) {
-                const uint32_t bits = static_cast<uint32_t>(sees >> (32 * t)) >> (4 * hi);
+                for (uint32_t t = 0; t < S::kSTiles; ++t) {
+                    const uint32_t bits = static_cast<uint32_t>(sees >> (32 * t)) >> (4 * hi);
 #pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) {
-                    float x = s[t][i] * factor;
-                    if (masked && !((bits >> (8 * (i >> 2) + (i & 3))) & 1u)) x = kLowest;
-                    s[t][i] = x;
-                    top = fmaxf(top, x);
+                    for (uint32_t i = 0; i < 16; ++i)
+                        s[t][i] = (bits >> (8 * (i >> 2) + (i & 3))) & 1u ? s[t][i] * factor : kLowest;
                 }
+                factor = 1.f;
             }
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
-            const float m2 = fmaxf(m, top);
-            const float base = m2 == kLowest ? 0.f : m2;  // no score above the lowest yet
-            const float shrink = __builtin_amdgcn_exp2f(m - base);
-            m = m2;
+            float top = s[0][0];
+#pragma unroll
+            for (uint32_t t = 0; t < S::kSTiles; ++t)
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+            top = fmaxf(top, __shfl_xor(top, 32, 64)) * factor;
+            // The sums keep their base until a score passes it by kSlack: weights
+            // are then at most 2^kSlack, which every type here holds, and the
+            // accumulators are seldom scaled (m below the base's row maximum
+            // by less than that only moves the common factor of l and o).
+            float grow = 1.f;
+            if (__any(top > m + kSlack)) {
+                const float m2 = fmaxf(m, top);
+                grow = m2 == kLowest ? 1.f : __builtin_amdgcn_exp2f(m - m2);
+                m = m2;
+                l *= grow;
+            }
+            const float base = m == kLowest ? 0.f : m;  // no score above the lowest yet
             float sum = 0.f;
             uint32_t p[S::kSTiles][8];
 #pragma unroll
             for (uint32_t t = 0; t < S::kSTiles; ++t)
 #pragma unroll
                 for (uint32_t i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(s[t][i] - base);
-                    const float y = __builtin_amdgcn_exp2f(s[t][i + 1] - base);
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[t][i], factor, -base));
+                    const float y = __builtin_amdgcn_exp2f(fmaf(s[t][i + 1], factor, -base));
                     sum += x + y;
                     p[t][i / 2] = T::pack(x, y);
                 }
-            l = l * shrink + sum;
-            float grow = shrink;
+            l += sum;
             if (kE4M3 && is_new && !scaled) {
                 grow *= value_scale;
                 scaled = true;
@@ -905,6 +921,8 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     a.max_pages = static_cast<uint32_t>(max_pages);
     a.q_heads = static_cast<uint32_t>(q_heads);
     a.group = static_cast<uint32_t>(q_heads / cache->heads);
+    a.page_shift = (cache->page_size & (cache->page_size - 1)) == 0
+                       ? static_cast<uint32_t>(__builtin_ctzll(cache->page_size)) : 32u;
     a.scale = scale;
     a.tile_keys = p.tile_keys;
     a.row_tile_rows = kRows * p.row_waves;
