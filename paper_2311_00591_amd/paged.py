@@ -15,9 +15,11 @@ transposed view, or one half of a tensor that holds keys and values together).
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import Optional
 
 import torch
+from torch._C import _cuda_getCurrentRawStream as _current_stream
 
 from . import COOP_EVICTABLE, COOP_PINNED, _check, _ptr, load_library
 
@@ -57,66 +59,75 @@ def _vector(t: torch.Tensor, name: str, dtype, device, *shape) -> torch.Tensor:
     return t
 
 
-def _strides(t: torch.Tensor, name: str, elements: int, count: int):
-    """The strides of the leading dimensions, of which one of size 1 or a
-    tensor without elements has none that matters."""
-    size, stride = t.shape, t.stride()
-    if t.numel() == 0:
-        return (0,) * count
-    if stride[-1] != 1 and size[-1] != 1:
+def _strides(t: torch.Tensor, name: str, elements: int):
+    """The strides of the leading dimensions (0 for one of size 1)."""
+    stride = t.stride()
+    if stride[-1] != 1 and t.shape[-1] != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    out = tuple(0 if size[i] == 1 else stride[i] for i in range(count))
-    if any(x % elements for x in out) or t.data_ptr() % 16:
-        raise ValueError(f"{name}'s rows must start at multiples of 16 bytes")
-    return out
+    bad = t.data_ptr() % 16
+    for x in stride[:-1]:
+        bad |= x % elements
+    if bad:  # (unless the offending dimension is one that is never stepped along)
+        stride = tuple(0 if n == 1 else x for n, x in zip(t.shape, stride))
+        if t.data_ptr() % 16 or any(x % elements for x in stride[:-1]):
+            raise ValueError(f"{name}'s rows must start at multiples of 16 bytes")
+    return stride[:-1]
 
 
-def _rows(t: torch.Tensor, name: str, dtype, device, tokens, heads, dim) -> CoopRows:
+def _rows(t: torch.Tensor, name: str, dtype, device, shape) -> CoopRows:
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.shape != (tokens, heads, dim):
-        raise ValueError(f"{name} must have shape {(tokens, heads, dim)}, got {tuple(t.shape)}")
-    return CoopRows(_ptr(t), _strides(t, name, 8, 2))
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {shape}, got {tuple(t.shape)}")
+    if shape[0] == 0:
+        return CoopRows(None, (0, 0))
+    return CoopRows(t.data_ptr(), _strides(t, name, 8))
 
 
 def _cache(k_cache, v_cache, k_scale, v_scale, dtype, device) -> CoopCache:
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape:
+    shape, kind = k_cache.shape, k_cache.dtype
+    if len(shape) != 4 or shape != v_cache.shape:
         raise ValueError("k_cache and v_cache must have one shape [pages, page_size, heads, dim], "
-                         f"got {tuple(k_cache.shape)} and {tuple(v_cache.shape)}")
-    kind = k_cache.dtype
+                         f"got {tuple(shape)} and {tuple(v_cache.shape)}")
     if v_cache.dtype != kind or kind not in (dtype, torch.float8_e4m3fn):
         raise TypeError(f"k_cache and v_cache must both be {dtype} or torch.float8_e4m3fn, got "
                         f"{kind} and {v_cache.dtype}")
     if k_cache.device != device or v_cache.device != device:
         raise ValueError(f"the cache is on {k_cache.device} and {v_cache.device}, expected {device}")
-    pages, page_size, heads, dim = k_cache.shape
-    elements = 8
+    pages, page_size, heads, dim = shape
+    elements, ks, vs = 8, None, None
     if kind == torch.float8_e4m3fn:
         elements = 16
         if k_scale is None or v_scale is None:
             raise ValueError("a float8_e4m3fn cache needs k_scale and v_scale")
-        _vector(k_scale, "k_scale", torch.float32, device, heads)
-        _vector(v_scale, "v_scale", torch.float32, device, heads)
+        ks = _vector(k_scale, "k_scale", torch.float32, device, heads).data_ptr()
+        vs = _vector(v_scale, "v_scale", torch.float32, device, heads).data_ptr()
     elif k_scale is not None or v_scale is not None:
         raise ValueError(f"a {kind} cache has no k_scale or v_scale")
-    return CoopCache(_ptr(k_cache), _ptr(v_cache), _strides(k_cache, "k_cache", elements, 3),
-                     _strides(v_cache, "v_cache", elements, 3),
-                     None if k_scale is None else k_scale.data_ptr(),
-                     None if v_scale is None else v_scale.data_ptr(),
-                     pages, page_size, heads, dim, _TYPES[kind])
+    if k_cache.numel() == 0:
+        return CoopCache(None, None, (0, 0, 0), (0, 0, 0), ks, vs, pages, page_size, heads, dim,
+                         _TYPES[kind])
+    return CoopCache(k_cache.data_ptr(), v_cache.data_ptr(), _strides(k_cache, "k_cache", elements),
+                     _strides(v_cache, "v_cache", elements), ks, vs, pages, page_size, heads, dim,
+                     _TYPES[kind])
 
 
-def _workspace(workspace: Optional[torch.Tensor], need: int, device) -> torch.Tensor:
+def _workspace(workspace: Optional[torch.Tensor], need: int, device, made):
+    """(the workspace to keep alive, its address, its bytes)."""
     if workspace is None:
-        return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+        if need == 0:
+            return None, None, 0
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        made.append(workspace)
+        return workspace, workspace.data_ptr(), need
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous memory on {device}")
-    if workspace.numel() * workspace.element_size() < need:
-        raise ValueError(f"workspace holds {workspace.numel() * workspace.element_size()} bytes, "
-                         f"needs {need}")
-    return workspace
+    held = workspace.numel() * workspace.element_size()
+    if held < need:
+        raise ValueError(f"workspace holds {held} bytes, needs {need}")
+    return workspace, workspace.data_ptr(), held
 
 
 class _Call:
@@ -130,20 +141,25 @@ class _Call:
     def launch(self, stream: Optional[int] = None) -> None:
         """Enqueues the call on `stream` (default: torch's current stream of
         the tensors' device)."""
+        index = self.device.index
+        current = _current_stream(index)
         if stream is None:
-            stream = torch.cuda.current_stream(self.device).cuda_stream
-        elif stream != torch.cuda.current_stream(self.device).cuda_stream:
+            stream = current
+        elif stream != current:
             # memory from torch's allocator is not reused before that stream is done with it
             other = torch.cuda.ExternalStream(stream, self.device)
             for t in self._made:
                 t.record_stream(other)
-        if torch.cuda.current_device() == self.device.index:
-            _check(self._fn(*self._args, stream))
+        if torch.cuda.current_device() == index:
+            status = self._fn(*self._args, stream)
         else:
             with torch.cuda.device(self.device):
-                _check(self._fn(*self._args, stream))
+                status = self._fn(*self._args, stream)
+        if status:
+            _check(status)
 
 
+@functools.lru_cache(maxsize=1024)
 def page_tables_workspace_size(num_pages: int, num_requests: int) -> int:
     """Device workspace bytes coop_page_tables needs."""
     out = ctypes.c_size_t(0)
@@ -184,22 +200,25 @@ class PageTables(_Call):
             raise ValueError(f"page_size must be at least 1, got {page_size}")
         if taken not in (COOP_EVICTABLE, COOP_PINNED):
             raise ValueError(f"taken must be COOP_EVICTABLE or COOP_PINNED, got {taken}")
-        made = []
         if out is None:
-            out = made = [torch.empty_like(t) for t in (table, held, kind)]
-        self.table = _vector(out[0], "out[0]", torch.int32, device, rows, cols)
-        self.held = _vector(out[1], "out[1]", torch.int32, device, rows)
-        self.kind = _vector(out[2], "out[2]", torch.uint8, device, pages)
-        words = torch.empty(2, dtype=torch.int64, device=device)
-        self.free, self.status = words[:1], words[1:].view(torch.int32)[:1]
-        self.workspace = _workspace(workspace, page_tables_workspace_size(pages, rows), device)
+            out = (torch.empty_like(table), torch.empty_like(held), torch.empty_like(kind))
+            made = list(out)
+        else:
+            made = []
+            _vector(out[0], "out[0]", torch.int32, device, rows, cols)
+            _vector(out[1], "out[1]", torch.int32, device, rows)
+            _vector(out[2], "out[2]", torch.uint8, device, pages)
+        self.table, self.held, self.kind = out
+        self.status = torch.empty(1, dtype=torch.int32, device=device)
+        self.free = torch.empty(1, dtype=torch.int64, device=device)
+        made += (self.status, self.free)
+        self.workspace, ws, ws_bytes = _workspace(
+            workspace, page_tables_workspace_size(pages, rows), device, made)
         self._inputs = (kind, table, held, lengths)
         self._prepare(device, load_library().coop_page_tables,
                       (_ptr(kind), pages, _ptr(table), rows, cols, _ptr(held), _ptr(lengths),
                        page_size, taken, _ptr(self.table), _ptr(self.held), _ptr(self.kind),
-                       self.status.data_ptr(), self.free.data_ptr(), self.workspace.data_ptr(),
-                       self.workspace.numel() * self.workspace.element_size()),
-                      [*made, words, self.workspace])
+                       self.status.data_ptr(), self.free.data_ptr(), ws, ws_bytes), made)
 
     def __call__(self, stream: Optional[int] = None):
         self.launch(stream)
@@ -270,14 +289,15 @@ class CacheWrite(_Call):
         if k.dim() != 3:
             raise ValueError(f"k must have shape [tokens, heads, dim], got {tuple(k.shape)}")
         cache = _cache(k_cache, v_cache, k_scale, v_scale, k.dtype, device)
-        n = k.shape[0]
-        rows = [_rows(t, name, k.dtype, device, n, cache.heads, cache.dim)
-                for t, name in ((k, "k"), (v, "v"))]
+        shape = n, _, _ = (k.shape[0], cache.heads, cache.dim)
+        k_rows = _rows(k, "k", k.dtype, device, shape)
+        v_rows = _rows(v, "v", k.dtype, device, shape)
         _vector(slots, "slots", torch.int64, device, n)
         self.k_cache, self.v_cache = k_cache, v_cache
         self._inputs = (k, v, slots, k_scale, v_scale)
         self._prepare(device, load_library().coop_cache_write,
-                      (*rows, _TYPES[k.dtype], _ptr(slots), n, cache), [])
+                      (ctypes.byref(k_rows), ctypes.byref(v_rows), _TYPES[k.dtype], _ptr(slots), n,
+                       ctypes.byref(cache)), [])
 
     def __call__(self, stream: Optional[int] = None):
         self.launch(stream)
@@ -290,6 +310,7 @@ def cache_write(k, v, slots, k_cache, v_cache, *, k_scale=None, v_scale=None,
     return CacheWrite(k, v, slots, k_cache, v_cache, k_scale=k_scale, v_scale=v_scale)(stream)
 
 
+@functools.lru_cache(maxsize=1024)
 def tree_attention_workspace_size(num_requests: int, num_tokens: int, q_heads: int, heads: int,
                                   dim: int) -> int:
     """Device workspace bytes coop_tree_attention needs."""
@@ -330,9 +351,9 @@ class TreeAttention(_Call):
         if cache.heads == 0 or q_heads == 0 or q_heads % cache.heads:
             raise ValueError(f"{q_heads} query heads cannot share {cache.heads} key/value heads")
         requests, cols = table.shape
-        rows = [_rows(t, name, q.dtype, device, n, heads, cache.dim)
-                for t, name, heads in ((q, "q", q_heads), (k, "k", cache.heads),
-                                       (v, "v", cache.heads))]
+        q_rows = _rows(q, "q", q.dtype, device, (n, q_heads, cache.dim))
+        k_rows = _rows(k, "k", q.dtype, device, (n, cache.heads, cache.dim))
+        v_rows = _rows(v, "v", q.dtype, device, (n, cache.heads, cache.dim))
         _vector(table, "table", torch.int32, device, requests, cols)
         _vector(lengths, "lengths", torch.int64, device, requests)
         _vector(token_offsets, "token_offsets", torch.int64, device, requests + 1)
@@ -342,20 +363,21 @@ class TreeAttention(_Call):
         if out is None:
             out = torch.empty((n, q_heads, dim), dtype=q.dtype, device=device)
             made.append(out)
-        self.out = _vector(out, "out", q.dtype, device, n, q_heads, dim)
-        need = tree_attention_workspace_size(requests, n, q_heads, cache.heads, dim)
-        if workspace is None:
-            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
-            made.append(workspace)
-        self.workspace = _workspace(workspace, need, device)
+        else:
+            _vector(out, "out", q.dtype, device, n, q_heads, dim)
+        self.out = out
+        self.workspace, ws, ws_bytes = _workspace(
+            workspace, tree_attention_workspace_size(requests, n, q_heads, cache.heads, dim),
+            device, made)
         self._inputs = (q, k, v, k_cache, v_cache, table, lengths, token_offsets, parents, k_scale,
                         v_scale)
         self._prepare(device, load_library().coop_tree_attention,
-                      (*rows, _TYPES[q.dtype], q_heads, n, token_offsets.data_ptr(),
-                       None if parents is None else _ptr(parents), cache, _ptr(table), cols,
-                       _ptr(lengths), requests, dim ** -0.5 if scale is None else float(scale),
-                       _ptr(self.out), self.workspace.data_ptr(),
-                       self.workspace.numel() * self.workspace.element_size()), made)
+                      (ctypes.byref(q_rows), ctypes.byref(k_rows), ctypes.byref(v_rows),
+                       _TYPES[q.dtype], q_heads, n, token_offsets.data_ptr(),
+                       None if parents is None else _ptr(parents), ctypes.byref(cache), _ptr(table),
+                       cols, _ptr(lengths), requests,
+                       dim ** -0.5 if scale is None else float(scale), _ptr(out), ws, ws_bytes),
+                      made)
 
     def __call__(self, stream: Optional[int] = None) -> torch.Tensor:
         self.launch(stream)

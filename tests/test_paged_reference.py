@@ -58,8 +58,8 @@ def _lib():
 
 def test_page_tables_refusals():
     def call(pages=8, rows=2, cols=4, page=16, taken=2, wsb=1 << 20, **ptr):
-        a = dict(kind=0x10000, table=0x20000, held=0x30000, lengths=0x40000, table_out=0x50000,
-                 held_out=0x60000, kind_out=0x70000, status=0x80000, free=0x90000, ws=0xa0000)
+        a = dict(kind=0x1000000, table=0x2000000, held=0x3000000, lengths=0x4000000,
+                 table_out=0x5000000, held_out=0x6000000, kind_out=0x7000000, status=0x8000000, free=0x9000000, ws=0xa000000)
         a.update(ptr)
         return _lib().coop_page_tables(a["kind"], pages, a["table"], rows, cols, a["held"],
                                        a["lengths"], page, taken, a["table_out"], a["held_out"],
@@ -68,18 +68,21 @@ def test_page_tables_refusals():
     for name in ("kind", "table", "held", "lengths", "table_out", "held_out", "kind_out", "status",
                  "free"):
         assert call(**{name: None}) == -1, name
-    assert call(ws=None) == -2 and call(wsb=8) == -2
+    # (a pool of up to 2^17 pages and 2^10 rows needs no workspace)
+    for large in (dict(pages=1 << 20), dict(rows=1025)):
+        assert call(ws=None, **large) == -2 and call(wsb=8, **large) == -2
     assert call(page=0) == -1 and call(taken=0) == -1 and call(taken=3) == -1
     for big in ("pages", "rows", "cols"):
         assert call(**{big: 1 << 31}) == -1, big
     # an output may be its own input, not another one or a part of one
-    assert call(table_out=0x20004) == -1
-    assert call(table_out=0x30000) == -1
-    assert call(kind_out=0x40000) == -1
+    assert call(table_out=0x2000004) == -1
+    assert call(table_out=0x3000000) == -1
+    assert call(kind_out=0x4000000) == -1
     out = ctypes.c_size_t()
     assert _lib().coop_page_tables_workspace_size(1, 1, None) == -1
     assert _lib().coop_page_tables_workspace_size(1 << 31, 1, ctypes.byref(out)) == -1
-    assert coop.page_tables_workspace_size(100000, 64) < 1 << 16
+    assert coop.page_tables_workspace_size(100000, 64) == 0
+    assert 0 < coop.page_tables_workspace_size(1 << 20, 64) < 1 << 16
 
 
 def test_slot_map_refusals():
