@@ -479,7 +479,8 @@ coop_status_t coop_cache_write(const coop_rows_t *k, const coop_rows_t *v, int32
  * flight at the same time must not share one.
  *
  * Keys and values written to the pool earlier on the same stream are seen.
- * num_tokens * q_heads and num_requests are at most 2^31 - 1.
+ * num_tokens * q_heads is at most 2^28, num_requests * cache->heads 2^22 and
+ * max_pages * page_size 2^31 - 1.
  */
 coop_status_t coop_tree_attention_workspace_size(uint64_t num_requests, uint64_t num_tokens,
                                                  uint64_t q_heads, uint64_t heads, uint64_t dim,

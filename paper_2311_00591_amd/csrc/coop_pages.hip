@@ -30,6 +30,7 @@ constexpr uint32_t kThreads = 256;
 constexpr uint32_t kTilePages = 4096;   // pages a workgroup counts or hands out
 constexpr uint32_t kScanThreads = 1024;
 constexpr uint32_t kMaxGrid = 1u << 16;
+constexpr uint32_t kLaneTokens = 4, kWaveTokens = 64 * kLaneTokens;  // of the slot map
 
 struct RowAsk {
     uint32_t first;  // entries that the row keeps
@@ -350,6 +351,10 @@ __global__ __launch_bounds__(kScanThreads) void pages_small_kernel(
 #pragma unroll
     for (uint32_t j = 0; j < kPageChunks; ++j) {
         const uint32_t c = j * kScanThreads + tid;
+        if (j * kScanThreads >= chunks) {  // (no such pages)
+            reinterpret_cast<uint16_t*>(free_bits)[c] = 0;
+            continue;
+        }
         const uint32_t words[4] = {kinds[j].x, kinds[j].y, kinds[j].z, kinds[j].w};
         uint32_t bits = 0;
 #pragma unroll
@@ -401,29 +406,33 @@ __global__ __launch_bounds__(kScanThreads) void pages_small_kernel(
     __syncthreads();
     const uint32_t granted = granted_rows;
     const uint64_t handed = granted ? row_upto[granted - 1] : 0;
-    // pages taken: a wavefront looks at 64 pages, a lane at one
-    for (uint32_t g = w; g < (pages + 63) / 64; g += kScanThreads / 64) {
-        const uint32_t base = group_rank[g];
-        if (base >= handed) break;
-        const uint64_t bits = free_bits[2 * g] | static_cast<uint64_t>(free_bits[2 * g + 1]) << 32;
-        const uint32_t r = base + __popcll(bits & ((1ull << lane) - 1));
-        const bool take = ((bits >> lane) & 1u) && r < handed;
-        const uint64_t took = __ballot(take);
-        if (lane == 0) {
-            taken_bits[2 * g] = static_cast<uint32_t>(took);
-            taken_bits[2 * g + 1] = static_cast<uint32_t>(took >> 32);
+    // pages taken: a thread takes 32 pages at a time; its first free one finds
+    // its row by search, the others go on from there
+    for (uint32_t i = tid; i < (pages + 31) / 32; i += kScanThreads) {
+        uint32_t r = group_rank[i >> 1] + (i & 1u ? __popc(free_bits[i - 1]) : 0u);
+        uint32_t bits = free_bits[i], took = 0;
+        if (!bits || r >= handed) continue;
+        uint32_t b = 0;
+        for (uint32_t hi = granted; b < hi;) {
+            const uint32_t mid = (b + hi) >> 1;
+            if (row_upto[mid] > r) hi = mid;
+            else b = mid + 1;
         }
-        if (take) {
-            uint32_t lo = 0, hi = granted;
-            while (lo < hi) {
-                const uint32_t mid = (lo + hi) >> 1;
-                if (row_upto[mid] > r) hi = mid;
-                else lo = mid + 1;
+        uint32_t upto = static_cast<uint32_t>(row_upto[b]);
+        uint32_t before = b ? static_cast<uint32_t>(row_upto[b - 1]) : 0;
+        int32_t* to = table_out + static_cast<uint64_t>(b) * cols + row_first[b];
+        for (; bits && r < handed; ++r) {
+            const uint32_t bit = __builtin_ctz(bits);
+            bits &= bits - 1;
+            took |= 1u << bit;
+            while (upto <= r) {  // (rows that ask for nothing are passed over)
+                before = upto;
+                upto = static_cast<uint32_t>(row_upto[++b]);
+                to = table_out + static_cast<uint64_t>(b) * cols + row_first[b];
             }
-            const uint32_t before = lo ? static_cast<uint32_t>(row_upto[lo - 1]) : 0;
-            table_out[static_cast<uint64_t>(lo) * cols + row_first[lo] + (r - before)] =
-                static_cast<int32_t>(64 * g + lane);
+            to[r - before] = static_cast<int32_t>(32 * i + bit);
         }
+        taken_bits[i] = took;
     }
     if (tid >= granted && tid < rows && count) {  // refused: nothing there
         for (uint32_t c = h; c < need; ++c) table_out[static_cast<uint64_t>(tid) * cols + c] = -1;
@@ -471,7 +480,7 @@ __global__ __launch_bounds__(kThreads) void pages_small_rows_kernel(
     }
 }
 
-// One wavefront takes 64 consecutive tokens at a time.  The requests of its
+// One wavefront takes 256 consecutive tokens at a time.  The requests of its
 // first and last token are found together, 64 probes at a time, and its lanes
 // search between the two: tokens of a prompt share their request, and single
 // tokens of 64 requests are six steps apart.
@@ -483,27 +492,51 @@ __global__ __launch_bounds__(kThreads) void slot_map_kernel(
     const uint32_t lane = threadIdx.x & 63u;
     const uint64_t wave = static_cast<uint64_t>(blockIdx.x) * (kThreads / 64) +
                           __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    for (uint64_t t0 = wave * 64; t0 < tokens; t0 += static_cast<uint64_t>(gridDim.x) * kThreads) {
-        const uint64_t t = t0 + lane, t1 = min(t0 + 63, tokens - 1);
-        uint32_t lo = first_past(offsets, rows + 1, t0, lane);
-        uint32_t hi = lo <= rows && offsets[lo] > t1 ? lo : first_past(offsets, rows + 1, t1, lane);
-        lo = first_past_between(offsets, lo, hi, t);
-        if (t >= tokens) continue;
-        int64_t slot = -1;
-        if (lo > 0 && lo <= rows) {
-            const uint32_t b = lo - 1;
-            const uint64_t length = lengths[b], behind = offsets[lo] - t;  // behind >= 1
-            if (behind <= length) {
-                const uint64_t pos = length - behind;
-                const uint64_t c = page_shift < 64 ? pos >> page_shift : pos / page;
-                if (c < in_use(held[b], cols)) {
-                    const int32_t p = table[static_cast<uint64_t>(b) * cols + c];
-                    if (static_cast<uint32_t>(p) < pages)
-                        slot = static_cast<int64_t>(static_cast<uint64_t>(p) * page + (pos - c * page));
+    for (uint64_t t0 = wave * kWaveTokens; t0 < tokens;
+         t0 += static_cast<uint64_t>(gridDim.x) * (kThreads / 64) * kWaveTokens) {
+        const uint64_t t1 = min(t0 + kWaveTokens, tokens) - 1;
+        const uint32_t first = first_past(offsets, rows + 1, t0, lane);
+        const uint32_t last = first <= rows && offsets[first] > t1 ? first : first_past(offsets, rows + 1, t1, lane);
+        // a lane's consecutive tokens: the first is searched for, the others
+        // mostly are of the same request
+        uint64_t t = t0 + lane * kLaneTokens;
+        if (t > t1) continue;
+        uint32_t at = first_past_between(offsets, first, last, t);
+        uint64_t end = 0, length = 0;
+        uint32_t used = 0;
+        const int32_t* row = table;
+        bool fresh = true;
+#pragma unroll
+        for (uint32_t i = 0; i < kLaneTokens; ++i, ++t) {
+            if (t > t1) break;
+            if (!fresh && end <= t) {
+                do ++at;
+                while (at <= rows && offsets[at] <= t);
+                fresh = true;
+            }
+            int64_t slot = -1;
+            if (at > 0 && at <= rows) {
+                if (fresh) {
+                    const uint32_t b = at - 1;
+                    end = offsets[at];
+                    length = lengths[b];
+                    used = in_use(held[b], cols);
+                    row = table + static_cast<uint64_t>(b) * cols;
+                    fresh = false;
+                }
+                const uint64_t behind = end - t;  // at least 1
+                if (behind <= length) {
+                    const uint64_t pos = length - behind;
+                    const uint64_t c = page_shift < 64 ? pos >> page_shift : pos / page;
+                    if (c < used) {
+                        const int32_t p = row[c];
+                        if (static_cast<uint32_t>(p) < pages)
+                            slot = static_cast<int64_t>(static_cast<uint64_t>(p) * page + (pos - c * page));
+                    }
                 }
             }
+            slots[t] = slot;
         }
-        slots[t] = slot;
     }
 }
 
@@ -733,7 +766,7 @@ coop_status_t coop_slot_map(const int32_t* table, uint64_t num_requests, uint64_
     if (!slots || !token_offsets) return COOP_ERR_INVALID;
     if (num_requests && (!held || !lengths)) return COOP_ERR_INVALID;
     if (num_requests && max_pages && !table) return COOP_ERR_INVALID;
-    hipLaunchKernelGGL(slot_map_kernel, dim3(grid_for(num_tokens, kThreads)), dim3(kThreads), 0,
+    hipLaunchKernelGGL(slot_map_kernel, dim3(grid_for(num_tokens, kThreads / 64 * kWaveTokens)), dim3(kThreads), 0,
                        static_cast<hipStream_t>(stream), table, static_cast<uint32_t>(num_requests),
                        static_cast<uint32_t>(max_pages), held, lengths, token_offsets, num_tokens,
                        page_size, shift_of(page_size), static_cast<uint32_t>(num_pages), slots);

@@ -19,8 +19,9 @@
 // turn and are joined at the end, so that few rows still keep four wavefronts'
 // loads under way.  Keys are cut into ranges where the requests alone would
 // leave compute units idle; the parts of cut ranges go to the workspace and a
-// second kernel joins them.  A small kernel ahead of both reads the lengths,
-// which only the device knows, and lists the items.
+// second kernel joins them.  Only the device knows the lengths: with up to 64
+// requests every wavefront makes the plan for itself, a request a lane; with
+// more a small kernel ahead lists the items.
 //
 // Operands.  Products are 32x32x16 matrix instructions with the keys as the
 // rows of the first one: its result then holds, in each lane, one query row
@@ -56,7 +57,7 @@ constexpr float kSlack = 8.f;  // how far, in powers of two, scores may pass the
 struct Item {  // rows [32 kRowWaves rt, ...) of a request and head, tiles [first, last)
     uint32_t request, row_tile, head, first, last;
     uint32_t part;  // where its result goes in the workspace; kWhole: to the output
-    uint32_t pad[2];
+    uint32_t pad[2];  // (32 bytes)
 };
 constexpr uint32_t kWhole = ~0u;
 
@@ -118,38 +119,126 @@ __device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
     return v;
 }
 
-// Lists the items.  All ranges are `chunk` tiles long, a length that gives
-// about `target` of them when the keys are spread evenly: with W tiles in all,
-// chunk >= W / target, so the rows that are cut make at most 2 target parts.
+// All ranges are `chunk` tiles long, a length that gives about `target` of them
+// when the keys are spread evenly: with W tiles in all, chunk >= W / target, so
+// the rows that are cut make at most 2 target parts.
+__device__ __forceinline__ uint32_t chunk_of(const Args& a, uint64_t work) {
+    const double even = ceil(static_cast<double>(work) / a.target);
+    const uint32_t n = even < 0x1p30 ? max(static_cast<uint32_t>(even), a.least) : 1u << 30;
+    return (n + a.chunk_multiple - 1) / a.chunk_multiple * a.chunk_multiple;
+}
+
+__device__ __forceinline__ uint32_t row_tiles_of(const Args& a, uint32_t tokens) {
+    return static_cast<uint32_t>((static_cast<uint64_t>(tokens) * a.group + a.row_tile_rows - 1) / a.row_tile_rows);
+}
+
+__device__ __forceinline__ uint32_t tiles_of(const Args& a, const Extent& e) {
+    return ceil_div(e.cached, a.tile_keys) + ceil_div(e.tokens, a.tile_keys);
+}
+
+__device__ __forceinline__ uint32_t scan_lanes(uint32_t v, uint32_t lane) {
+    for (uint32_t d = 1; d < 64; d <<= 1) {
+        const uint32_t up = __shfl_up(v, d, 64);
+        if (lane >= d) v += up;
+    }
+    return v;
+}
+
+// The plan of at most 64 requests, which every wavefront makes for itself: a
+// lane holds a request's numbers.
+struct LanePlan {
+    Extent e;
+    uint32_t chunk, tiles, pairs, ranges;
+    uint32_t items, cuts, joins;  // running sums, this request's included
+};
+
+__device__ __forceinline__ LanePlan lane_plan(const Args& a, uint32_t lane) {
+    LanePlan p;
+    p.e = Extent{0, 0, 0};
+    if (lane < a.requests) p.e = extent(a, lane);
+    const uint32_t heads = static_cast<uint32_t>(a.cache.heads);
+    p.tiles = p.e.tokens ? tiles_of(a, p.e) : 0;
+    p.pairs = row_tiles_of(a, p.e.tokens) * heads;
+    p.chunk = chunk_of(a, wave_sum(static_cast<uint64_t>(p.pairs) * p.tiles));
+    p.ranges = ceil_div(p.tiles, p.chunk);
+    const bool cut = p.ranges > 1;
+    p.items = scan_lanes(p.pairs * p.ranges, lane);
+    p.cuts = scan_lanes(cut ? p.pairs * p.ranges : 0, lane);
+    p.joins = scan_lanes(cut ? p.pairs : 0, lane);
+    return p;
+}
+
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, uint32_t lane) {
+    return __builtin_amdgcn_readlane(v, lane);
+}
+
+__device__ __forceinline__ Extent extent_of(const LanePlan& p, uint32_t r) {
+    Extent e;
+    e.first = from_lane(static_cast<uint32_t>(p.e.first), r) |
+              static_cast<uint64_t>(from_lane(static_cast<uint32_t>(p.e.first >> 32), r)) << 32;
+    e.tokens = from_lane(p.e.tokens, r);
+    e.cached = from_lane(p.e.cached, r);
+    return e;
+}
+
+// Item i of the plan; false if it has no such item.
+__device__ __forceinline__ bool item_of(const Args& a, const LanePlan& p, uint32_t i, Item* it,
+                                        Extent* e) {
+    const uint64_t past = __ballot(p.items > i);
+    if (!past) return false;
+    const uint32_t r = static_cast<uint32_t>(__builtin_ctzll(past));
+    const uint32_t pairs = from_lane(p.pairs, r), ranges = from_lane(p.ranges, r);
+    const uint32_t j = i - (from_lane(p.items, r) - pairs * ranges);
+    const uint32_t c = j / pairs, pair = j - c * pairs, heads = static_cast<uint32_t>(a.cache.heads);
+    *e = extent_of(p, r);
+    it->request = r;
+    it->row_tile = pair / heads;
+    it->head = pair - it->row_tile * heads;
+    it->first = c * p.chunk;
+    it->last = min(from_lane(p.tiles, r), it->first + p.chunk);
+    it->part = ranges > 1 ? from_lane(p.cuts, r) - pairs * ranges + pair * ranges + c : kWhole;
+    return true;
+}
+
+__device__ __forceinline__ void join_of(const Args& a, const LanePlan& p, uint32_t i, Join* jn,
+                                        Extent* e) {
+    const uint32_t r = static_cast<uint32_t>(__builtin_ctzll(__ballot(p.joins > i)));
+    const uint32_t pairs = from_lane(p.pairs, r), heads = static_cast<uint32_t>(a.cache.heads);
+    const uint32_t pair = i - (from_lane(p.joins, r) - pairs);
+    *e = extent_of(p, r);
+    jn->request = r;
+    jn->row_tile = pair / heads;
+    jn->head = pair - jn->row_tile * heads;
+    jn->parts = from_lane(p.ranges, r);
+    jn->first = from_lane(p.cuts, r) - pairs * jn->parts + pair * jn->parts;
+}
+
+// More requests: one workgroup lists the items and the joins.
 __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
     __shared__ uint64_t part[kPlanThreads / 64][3];
     __shared__ uint32_t item_base[kPlanThreads + 1], cut_base[kPlanThreads], join_base[kPlanThreads + 1];
-    __shared__ uint32_t row_tiles_of[kPlanThreads], tiles_of[kPlanThreads];
+    __shared__ uint32_t request_rows[kPlanThreads], request_tiles[kPlanThreads];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, w = tid >> 6;
     const uint32_t heads = static_cast<uint32_t>(a.cache.heads);
     uint64_t work = 0;
     for (uint32_t b = tid; b < a.requests; b += kPlanThreads) {
         const Extent e = extent(a, b);
-        const uint64_t rt = (static_cast<uint64_t>(e.tokens) * a.group + a.row_tile_rows - 1) / a.row_tile_rows;
-        work += rt * heads * (ceil_div(e.cached, a.tile_keys) + ceil_div(e.tokens, a.tile_keys));
+        work += static_cast<uint64_t>(row_tiles_of(a, e.tokens)) * heads * tiles_of(a, e);
     }
     work = wave_sum(work);
     if (lane == 0) part[w][0] = work;
     __syncthreads();
     work = 0;
     for (uint32_t i = 0; i < kPlanThreads / 64; ++i) work += part[i][0];
-    uint64_t chunk64 = max((work + a.target - 1) / a.target, static_cast<uint64_t>(a.least));
-    chunk64 = (chunk64 + a.chunk_multiple - 1) / a.chunk_multiple * a.chunk_multiple;
-    const uint32_t chunk = static_cast<uint32_t>(min(chunk64, static_cast<uint64_t>(1u << 30)));
+    const uint32_t chunk = chunk_of(a, work);
     uint32_t items0 = 0, cuts0 = 0, joins0 = 0;  // of the requests before this batch
     for (uint32_t b0 = 0; b0 < a.requests; b0 += kPlanThreads) {
         const uint32_t b = b0 + tid;
         uint32_t tiles = 0, rt = 0;
         if (b < a.requests) {
             const Extent e = extent(a, b);
-            rt = static_cast<uint32_t>(
-                (static_cast<uint64_t>(e.tokens) * a.group + a.row_tile_rows - 1) / a.row_tile_rows);
-            tiles = ceil_div(e.cached, a.tile_keys) + ceil_div(e.tokens, a.tile_keys);
+            rt = row_tiles_of(a, e.tokens);
+            tiles = tiles_of(a, e);
         }
         const uint32_t pairs = rt * heads, ranges = ceil_div(tiles, chunk);
         const uint64_t mine[3] = {static_cast<uint64_t>(pairs) * ranges,
@@ -177,8 +266,8 @@ __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
         item_base[tid] = static_cast<uint32_t>(min(sum[0] - mine[0], static_cast<uint64_t>(kWhole)));
         cut_base[tid] = static_cast<uint32_t>(sum[1] - mine[1]);
         join_base[tid] = static_cast<uint32_t>(sum[2] - mine[2]);
-        row_tiles_of[tid] = rt;
-        tiles_of[tid] = tiles;
+        request_rows[tid] = rt;
+        request_tiles[tid] = tiles;
         if (tid == kPlanThreads - 1) {
             item_base[kPlanThreads] = static_cast<uint32_t>(min(sum[0], static_cast<uint64_t>(kWhole)));
             join_base[kPlanThreads] = static_cast<uint32_t>(sum[2]);
@@ -192,9 +281,9 @@ __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
                 if (item_base[mid] <= i) lo = mid;
                 else hi = mid;
             }
-            const uint32_t j = i - item_base[lo], p = row_tiles_of[lo] * heads;
+            const uint32_t j = i - item_base[lo], p = request_rows[lo] * heads;
             const uint32_t c = j / p, pair = j - c * p;
-            const uint32_t t = tiles_of[lo], r = ceil_div(t, chunk);
+            const uint32_t t = request_tiles[lo], r = ceil_div(t, chunk);
             Item it;
             it.request = b0 + lo;
             it.row_tile = pair / heads;
@@ -212,7 +301,7 @@ __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
                 if (join_base[mid] <= i) lo = mid;
                 else hi = mid;
             }
-            const uint32_t pair = i - join_base[lo], r = ceil_div(tiles_of[lo], chunk);
+            const uint32_t pair = i - join_base[lo], r = ceil_div(request_tiles[lo], chunk);
             Join jn;
             jn.request = b0 + lo;
             jn.row_tile = pair / heads;
@@ -314,9 +403,18 @@ __device__ __forceinline__ uint32_t value_chunk(uint32_t r, uint32_t c) {
     return kDim == 64 ? c ^ (((r >> 1) & 1u) << 2) : c ^ ((r & 3u) << 2);
 }
 
+// Device memory by name: a load through a pointer that itself comes from LDS
+// would otherwise be one that may mean LDS, and every wait for LDS would wait
+// for it too.
+typedef const __attribute__((address_space(1))) uint8_t* Global;
+
+__device__ __forceinline__ u32x4 load16(Global p) {
+    return *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(p);
+}
+
 struct RowAt {  // where a tile's key and value rows are in memory
-    const uint8_t* k;
-    const uint8_t* v;
+    Global k;
+    Global v;
 };
 
 template <class T, bool kE4M3, uint32_t kDim, uint32_t kRowWaves>
@@ -330,9 +428,16 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     __shared__ uint32_t odd;                      // whether new values are not all finite
     __shared__ float joined[4][kRows][2];
 
-    if (blockIdx.x >= a.head->items) return;
-    const Item item = a.items[blockIdx.x];
     const uint32_t tid = threadIdx.x, lane = tid & 63u;
+    Item item;
+    Extent e;
+    if (a.requests <= 64) {
+        if (!item_of(a, lane_plan(a, lane), blockIdx.x, &item, &e)) return;
+    } else {
+        if (blockIdx.x >= a.head->items) return;
+        item = a.items[blockIdx.x];
+        e = extent(a, item.request);
+    }
     const uint32_t w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t group = w / kRowWaves, row_wave = w % kRowWaves;
     const uint32_t gtid = tid - group * S::kGroupThreads;
@@ -341,7 +446,6 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     const uint32_t page_size = static_cast<uint32_t>(a.cache.page_size);
     const bool alike = a.cache.k_stride[0] == a.cache.v_stride[0] && a.cache.k_stride[1] == a.cache.v_stride[1];
     auto page_at = [&](uint32_t pos) { return a.page_shift < 32 ? pos >> a.page_shift : pos / page_size; };
-    const Extent e = extent(a, item.request);
     const uint32_t rows = e.tokens * a.group;
     const uint32_t row0 = item.row_tile * (kRows * kRowWaves);
     const uint32_t row = row0 + row_wave * kRows + n;
@@ -362,7 +466,20 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     if (in_lds)
         for (uint32_t i = tid; i < e.tokens; i += kThreads) tree[i] = a.parents[e.first + i];
     if (tid == 0) odd = 0;
-    __syncthreads();
+    // the rows' queries, permuted as the keys are
+    uint8_t* const query_tile = queries + row_wave * kRows * kDim * 2;
+    if (group == 0) {
+        const uint16_t* const base = static_cast<const uint16_t*>(a.q.data) +
+                                     (e.first + token) * a.q.stride[0] + qh * a.q.stride[1];
+#pragma unroll
+        for (uint32_t c = 0; c < kDim / 16; ++c) {
+            const uint32_t d = 16 * c + 8 * hi;
+            u32x4 x = {0, 0, 0, 0};
+            if (row_lives && d < dim) x = *reinterpret_cast<const u32x4*>(base + d);
+            *reinterpret_cast<u32x4*>(query_tile + (n * S::kChunks + key_chunk<kDim>(n, 2 * c + hi)) * 16) = x;
+        }
+    }
+    __syncthreads();  // (all groups read the queries, which the first one writes)
     const int32_t* const parents = a.parents ? a.parents + e.first : nullptr;
     auto parent_of = [&](int32_t i) { return in_lds ? tree[i] : parents[i]; };
 
@@ -389,19 +506,6 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     };
     start();
 
-    // the rows' queries, permuted as the keys are
-    uint8_t* const query_tile = queries + row_wave * kRows * kDim * 2;
-    if (group == 0) {
-        const uint16_t* const base = static_cast<const uint16_t*>(a.q.data) +
-                                     (e.first + token) * a.q.stride[0] + qh * a.q.stride[1];
-#pragma unroll
-        for (uint32_t c = 0; c < kDim / 16; ++c) {
-            const uint32_t d = 16 * c + 8 * hi;
-            u32x4 x = {0, 0, 0, 0};
-            if (row_lives && d < dim) x = *reinterpret_cast<const u32x4*>(base + d);
-            *reinterpret_cast<u32x4*>(query_tile + (n * S::kChunks + key_chunk<kDim>(n, 2 * c + hi)) * 16) = x;
-        }
-    }
     f32x16 o[S::kDTiles];
 #pragma unroll
     for (uint32_t t = 0; t < S::kDTiles; ++t)
@@ -415,10 +519,10 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     bool scaled = false;  // whether o has met the cached values' scale
 
     // rows that do not count are read from a place that is there and left out
-    const uint8_t* const spare = static_cast<const uint8_t*>(a.q.data);
+    const Global spare = (Global)(a.q.data);
     const uint64_t size = kE4M3 ? 1 : 2;
-    const uint8_t* const ck = static_cast<const uint8_t*>(a.cache.k) + item.head * a.cache.k_stride[2] * size;
-    const uint8_t* const cv = static_cast<const uint8_t*>(a.cache.v) + item.head * a.cache.v_stride[2] * size;
+    const Global ck = (Global)(a.cache.k) + item.head * a.cache.k_stride[2] * size;
+    const Global cv = (Global)(a.cache.v) + item.head * a.cache.v_stride[2] * size;
 
     // A tile's page number for lane's key (lanes past the tile repeat it).
     const uint32_t my_key = lane % kKeys;
@@ -444,10 +548,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
             const uint32_t j = (cached_tiles + new_tiles - 1 - tile) * kKeys + my_key;
             counts = j < e.tokens;
             if (counts) {
-                r.k = reinterpret_cast<const uint8_t*>(static_cast<const uint16_t*>(a.k.data) +
-                                                       (e.first + j) * a.k.stride[0] + item.head * a.k.stride[1]);
-                r.v = reinterpret_cast<const uint8_t*>(static_cast<const uint16_t*>(a.v.data) +
-                                                       (e.first + j) * a.v.stride[0] + item.head * a.v.stride[1]);
+                r.k = (Global)(a.k.data) + ((e.first + j) * a.k.stride[0] + item.head * a.k.stride[1]) * 2;
+                r.v = (Global)(a.v.data) + ((e.first + j) * a.v.stride[0] + item.head * a.v.stride[1]) * 2;
             }
         }
         if (lane < kKeys) rows_at[w][my_key] = r;
@@ -467,16 +569,16 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
 #pragma unroll
             for (uint32_t j = 0; j < kLoads8; ++j) {
                 const RowAt r = rows_at[w][row_of_load8 + j * kRowStep8];
-                kreg[j] = *reinterpret_cast<const u32x4*>(r.k + byte);
-                vreg[j] = *reinterpret_cast<const u32x4*>(r.v + byte);
+                kreg[j] = load16(r.k + byte);
+                vreg[j] = load16(r.v + byte);
             }
         } else {
             const uint32_t byte = chunk * 8 < dim ? chunk * 16 : 0;
 #pragma unroll
             for (uint32_t j = 0; j < kLoads; ++j) {
                 const RowAt r = rows_at[w][row_of_load + j * kRowStep];
-                kreg[j] = *reinterpret_cast<const u32x4*>(r.k + byte);
-                vreg[j] = *reinterpret_cast<const u32x4*>(r.v + byte);
+                kreg[j] = load16(r.k + byte);
+                vreg[j] = load16(r.v + byte);
             }
         }
     };
@@ -764,42 +866,75 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     }
 }
 
-// Joins the parts of rows whose keys were cut: one wavefront a row.
-template <class T, uint32_t kDim>
+// Joins the parts of rows whose keys were cut.  A row's parts are dealt to
+// kWaves wavefronts: four (a workgroup a row) where there are few rows and so
+// many parts, one where there are many rows.
+template <class T, uint32_t kDim, uint32_t kWaves>
 __global__ __launch_bounds__(kThreads) void attention_join_kernel(Args a) {
-    constexpr uint32_t kEach = kDim / 64;
+    constexpr uint32_t kEach = kDim / 64, kRowsAtOnce = 4 / kWaves;
+    __shared__ float sums[4][kDim + 64];
     const uint32_t lane = threadIdx.x & 63u;
     const uint32_t w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint64_t all = static_cast<uint64_t>(a.head->joins) * a.part_rows;
-    for (uint64_t i = blockIdx.x * 4ull + w; i < all; i += gridDim.x * 4ull) {
-        const Join j = a.joins[i / a.part_rows];
-        const uint32_t r = static_cast<uint32_t>(i % a.part_rows);
-        const Extent e = extent(a, j.request);
+    const bool few = a.requests <= 64;
+    LanePlan plan;
+    if (few) plan = lane_plan(a, lane);
+    const uint64_t joins = few ? from_lane(plan.joins, 63) : a.head->joins;
+    const uint32_t dim = static_cast<uint32_t>(a.cache.dim);
+    for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * kRowsAtOnce + (kWaves == 1 ? w : 0);
+         i < joins * a.part_rows; i += static_cast<uint64_t>(gridDim.x) * kRowsAtOnce) {
+        const uint32_t pair = static_cast<uint32_t>(i / a.part_rows);
+        const uint32_t r = static_cast<uint32_t>(i - static_cast<uint64_t>(pair) * a.part_rows);
+        Join j;
+        Extent e;
+        if (few) {
+            join_of(a, plan, pair, &j, &e);
+        } else {
+            j = a.joins[pair];
+            e = extent(a, j.request);
+        }
         const uint32_t row = j.row_tile * a.row_tile_rows + r;
         if (row >= e.tokens * a.group) continue;
         const uint32_t token = row / a.group, qh = j.head * a.group + row % a.group;
-        const uint64_t first = static_cast<uint64_t>(j.first) * a.part_rows + r;
+        const float2* const part_sum = a.part_sum + static_cast<uint64_t>(j.first) * a.part_rows + r;
+        const float* const part_out =
+            a.part_out + (static_cast<uint64_t>(j.first) * a.part_rows + r) * kDim + lane * kEach;
         float m = kLowest;
-        for (uint32_t p = lane; p < j.parts; p += 64)
-            m = fmaxf(m, a.part_sum[first + static_cast<uint64_t>(p) * a.part_rows].x);
+        for (uint32_t p = lane; p < j.parts; p += 64) m = fmaxf(m, part_sum[static_cast<uint64_t>(p) * a.part_rows].x);
         for (uint32_t d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
         const float base = m == kLowest ? 0.f : m;
         float l = 0.f, o[kEach];
+#pragma unroll
         for (uint32_t c = 0; c < kEach; ++c) o[c] = 0.f;
-        for (uint32_t p = 0; p < j.parts; ++p) {
-            const uint64_t at = first + static_cast<uint64_t>(p) * a.part_rows;
-            const float2 ml = a.part_sum[at];
+#pragma unroll 4
+        for (uint32_t p = kWaves == 1 ? 0 : w; p < j.parts; p += kWaves) {
+            const float2 ml = part_sum[static_cast<uint64_t>(p) * a.part_rows];
             const float x = __builtin_amdgcn_exp2f(ml.x - base);
             l += ml.y * x;
-            for (uint32_t c = 0; c < kEach; ++c) o[c] += a.part_out[at * kDim + lane * kEach + c] * x;
+#pragma unroll
+            for (uint32_t c = 0; c < kEach; ++c)
+                o[c] += part_out[static_cast<uint64_t>(p) * a.part_rows * kDim + c] * x;
+        }
+        if (kWaves > 1) {
+#pragma unroll
+            for (uint32_t c = 0; c < kEach; ++c) sums[w][lane * kEach + c] = o[c];
+            if (lane == 0) sums[w][kDim] = l;
+            __syncthreads();
+#pragma unroll
+            for (uint32_t c = 0; c < kEach; ++c) {
+                const uint32_t d = lane * kEach + c;
+                o[c] = (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]);
+            }
+            l = (sums[0][kDim] + sums[1][kDim]) + (sums[2][kDim] + sums[3][kDim]);
+            __syncthreads();
+            if (w) continue;
         }
         bool is_void = false;
         if (a.parents) {
             const int32_t p = a.parents[e.first + token];
             is_void = p < -1 || p >= static_cast<int32_t>(token);
         }
-        const uint32_t dim = static_cast<uint32_t>(a.cache.dim);
         uint16_t* const to = a.out + ((e.first + token) * a.q_heads + qh) * dim;
+#pragma unroll
         for (uint32_t c = 0; c < kEach; ++c)
             if (lane * kEach + c < dim)
                 to[lane * kEach + c] =
@@ -813,11 +948,14 @@ __global__ __launch_bounds__(kThreads) void attention_join_kernel(Args a) {
 
 constexpr uint64_t kMost = (1ull << 31) - 1;
 
+// (a launch has fewer than 2^32 threads, 256 an item)
+constexpr uint64_t kMostRows = 1ull << 28, kMostPairs = 1ull << 22;
+
 bool counts_valid(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t heads,
                   uint64_t dim) {
     return heads && heads <= coop_pages::kMaxHeads && q_heads && q_heads <= coop_pages::kMaxHeads &&
            q_heads % heads == 0 && requests < kMost && tokens <= kMost &&
-           tokens * q_heads <= kMost && requests * heads <= kMost && dim &&
+           tokens * q_heads <= kMostRows && requests * heads <= kMostPairs && dim &&
            dim <= coop_pages::kMaxDim && dim % 8 == 0;
 }
 
@@ -859,8 +997,12 @@ void launch(const Plan& p, const Args& a, uint32_t joins, hipStream_t s) {
                   : p.row_waves == 2 ? tree_attention_kernel<T, kE4M3, kDim, 2>
                                      : tree_attention_kernel<T, kE4M3, kDim, 4>;
     hipLaunchKernelGGL(kernel, dim3(a.max_items), dim3(kThreads), 0, s, a);
-    if (joins)
-        hipLaunchKernelGGL((attention_join_kernel<T, kDim>), dim3(joins), dim3(kThreads), 0, s, a);
+    if (joins) {
+        // the rows of all pairs: fewer than the device has wavefronts, or more
+        auto join = p.pairs * p.part_rows <= 1024 ? attention_join_kernel<T, kDim, 4>
+                                                  : attention_join_kernel<T, kDim, 1>;
+        hipLaunchKernelGGL(join, dim3(joins), dim3(kThreads), 0, s, a);
+    }
 }
 
 template <class T, bool kE4M3>
@@ -943,10 +1085,12 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     a.part_out = reinterpret_cast<float*>(ws + p.out_offset);
     // rows can be cut only if one can have more tiles than the shortest range
     const uint64_t join_rows = static_cast<uint64_t>(a.target) * a.part_rows;
-    const uint32_t joins = tiles > a.least ? static_cast<uint32_t>(join_rows / 4 < 2048 ? join_rows / 4 + 1 : 2048) : 0;
+    const uint32_t joins = tiles > a.least ? static_cast<uint32_t>(join_rows < 2048 ? join_rows : 2048) : 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipLaunchKernelGGL(attention_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
-    if (hipGetLastError() != hipSuccess) return COOP_ERR_HIP;
+    if (num_requests > 64) {
+        hipLaunchKernelGGL(attention_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+        if (hipGetLastError() != hipSuccess) return COOP_ERR_HIP;
+    }
     const bool e4m3 = cache->type == COOP_E4M3;
     if (type == COOP_BF16) {
         if (e4m3) launch_dim<Bf16, true>(p, a, joins, s);

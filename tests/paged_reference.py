@@ -9,7 +9,7 @@ E4M3_MAX = 448.0
 
 def page_tables(kind, table, held, lengths, page_size, taken=2):
     """(table, held, kind, status, free) as numpy arrays."""
-    kind, table = np.array(kind, dtype=np.uint8), np.array(table, dtype=np.int32)
+    kind, table = np.asarray(kind).astype(np.uint8), np.asarray(table).astype(np.int32)
     rows, cols = table.shape
     held = [min(max(int(h), 0), cols) for h in held]
     need = [-(-(int(n) % 2**64) // page_size) for n in lengths]
@@ -79,9 +79,10 @@ def seen(parents, i):
 
 
 def attention(q, k, v, k_cache, v_cache, table, lengths, offsets, parents, scale, k_scale=None,
-              v_scale=None):
+              v_scale=None, only=None):
     """out, and how far a result of q's type may be from it, both [tokens,
-    q_heads, dim] in 64 bits; rows of no request are NaN.
+    q_heads, dim] in 64 bits; rows of no request are NaN, and so are tokens not
+    in `only` (request-local numbers) where it is given.
 
     With u = eps / 2 of the type (half a step, relative) and w the exact
     weights, A = sum_j w_j |v_j|:
@@ -117,7 +118,7 @@ def attention(q, k, v, k_cache, v_cache, table, lengths, offsets, parents, scale
         at = [(p, o) for p, o in at if 0 <= p < pages]
         p, o = [x[0] for x in at], [x[1] for x in at]
         own = None if parents is None else parents[lo:hi].tolist()
-        for i in range(hi - lo):
+        for i in range(hi - lo) if only is None else only:
             tokens = seen(own, i)
             if tokens is None:
                 out[lo + i] = tol[lo + i] = 0

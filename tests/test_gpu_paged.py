@@ -337,6 +337,39 @@ def test_tree_attention_long(lengths, counts, heads, page, dtype, cache):
     _check_attention(a, coop.tree_attention(**a))
 
 
+@pytest.mark.parametrize("requests, longest, width, q_heads, heads", [
+    (64, 9000, 1, 32, 8), (8, 5000, 40, 16, 4), (100, 2000, 3, 8, 8), (3, 3500, 700, 8, 2)])
+def test_tree_attention_fills_the_device(requests, longest, width, q_heads, heads):
+    """Many workgroups at once: every run gives the same bits, and rows picked
+    at random are right."""
+    coop = _coop()
+    _announce(f"attention, {requests} requests up to {longest} + {width}")
+    rng = np.random.default_rng(requests)
+    lengths = rng.integers(1, longest, requests).tolist()
+    counts = rng.integers(1, width + 1, requests).tolist()
+    dim, page = 128, 16
+    a = _attention_inputs(requests, lengths, counts, q_heads, heads, dim, BF16, BF16, page,
+                          "tree" if width < 100 else None)
+    got = coop.tree_attention(**a)
+    for _ in range(4):
+        assert torch.equal(coop.tree_attention(**a), got)
+    offsets = np.concatenate([[0], np.cumsum(counts)])
+    for b in rng.permutation(requests)[:3]:
+        lo, hi = offsets[b], offsets[b + 1]
+        one = {**a, "table": a["table"][b:b + 1], "lengths": a["lengths"][b:b + 1],
+               "token_offsets": _ints([0, hi - lo])}
+        pick = sorted({0, hi - lo - 1})
+        for n in "qkv":
+            one[n] = a[n][lo:hi]
+        if a["parents"] is not None:
+            one["parents"] = a["parents"][lo:hi]
+        want, tol = ref.attention(one["q"], one["k"], one["v"], a["k_cache"], a["v_cache"], one["table"],
+                                  one["lengths"], one["token_offsets"], one["parents"], dim ** -0.5,
+                                  only=pick)
+        off = np.abs(got[lo:hi].double().cpu().numpy() - want)[pick]
+        assert (off <= tol[pick]).all(), (b, (off / tol[pick]).max())
+
+
 def test_tree_attention_long_chain_written_out():
     """parents of a chain give what parents=None gives, bit for bit."""
     coop = _coop()
