@@ -82,6 +82,10 @@ struct Args {
     uint64_t tokens;
     uint32_t requests, max_pages, q_heads, group;
     uint32_t page_shift;  // page_size is 2^page_shift; 32: not a power of two
+    // keys' and values' rows lie alike, and a row's offset is 32-bit products
+    // of these
+    bool narrow;
+    uint32_t page_bytes, place_bytes;
     float scale;
     // the plan and the workspace
     uint32_t tile_keys, row_tile_rows, target, least, chunk_multiple, max_items, part_rows;
@@ -172,6 +176,22 @@ __device__ __forceinline__ uint32_t from_lane(uint32_t v, uint32_t lane) {
     return __builtin_amdgcn_readlane(v, lane);
 }
 
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// The item and its request as scalars.
+__device__ __forceinline__ Item uniform(const Item& i) {
+    return {uniform(i.request), uniform(i.row_tile), uniform(i.head), uniform(i.first),
+            uniform(i.last), uniform(i.part), {0, 0}};
+}
+__device__ __forceinline__ Extent uniform(const Extent& e) {
+    Extent r;
+    r.first = uniform(static_cast<uint32_t>(e.first)) |
+              static_cast<uint64_t>(uniform(static_cast<uint32_t>(e.first >> 32))) << 32;
+    r.tokens = uniform(e.tokens);
+    r.cached = uniform(e.cached);
+    return r;
+}
+
 __device__ __forceinline__ Extent extent_of(const LanePlan& p, uint32_t r) {
     Extent e;
     e.first = from_lane(static_cast<uint32_t>(p.e.first), r) |
@@ -179,6 +199,15 @@ __device__ __forceinline__ Extent extent_of(const LanePlan& p, uint32_t r) {
     e.tokens = from_lane(p.e.tokens, r);
     e.cached = from_lane(p.e.cached, r);
     return e;
+}
+
+// Consecutive workgroups go to the eight dies in turn, and consecutive items to
+// consecutive heads.  Heads that lie side by side in a pool's rows are in few
+// of a die's cache channels each, so a die that met one head only would work
+// with these; the heads are turned from one row tile, range and request to the
+// next.
+__device__ __forceinline__ uint32_t turned(uint32_t head, uint32_t by, uint32_t heads) {
+    return (head + by % heads) % heads;
 }
 
 // Item i of the plan; false if it has no such item.
@@ -189,13 +218,14 @@ __device__ __forceinline__ bool item_of(const Args& a, const LanePlan& p, uint32
     const uint32_t r = static_cast<uint32_t>(__builtin_ctzll(past));
     const uint32_t pairs = from_lane(p.pairs, r), ranges = from_lane(p.ranges, r);
     const uint32_t j = i - (from_lane(p.items, r) - pairs * ranges);
-    const uint32_t c = j / pairs, pair = j - c * pairs, heads = static_cast<uint32_t>(a.cache.heads);
+    const uint32_t c = j / pairs, k = j - c * pairs, heads = static_cast<uint32_t>(a.cache.heads);
     *e = extent_of(p, r);
     it->request = r;
-    it->row_tile = pair / heads;
-    it->head = pair - it->row_tile * heads;
+    it->row_tile = k / heads;
+    it->head = turned(k - it->row_tile * heads, r + c + it->row_tile, heads);
     it->first = c * p.chunk;
     it->last = min(from_lane(p.tiles, r), it->first + p.chunk);
+    const uint32_t pair = it->row_tile * heads + it->head;
     it->part = ranges > 1 ? from_lane(p.cuts, r) - pairs * ranges + pair * ranges + c : kWhole;
     return true;
 }
@@ -282,14 +312,15 @@ __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
                 else hi = mid;
             }
             const uint32_t j = i - item_base[lo], p = request_rows[lo] * heads;
-            const uint32_t c = j / p, pair = j - c * p;
+            const uint32_t c = j / p, k = j - c * p;
             const uint32_t t = request_tiles[lo], r = ceil_div(t, chunk);
             Item it;
             it.request = b0 + lo;
-            it.row_tile = pair / heads;
-            it.head = pair - it.row_tile * heads;
+            it.row_tile = k / heads;
+            it.head = turned(k - it.row_tile * heads, it.request + c + it.row_tile, heads);
             it.first = c * chunk;
             it.last = min(t, it.first + chunk);
+            const uint32_t pair = it.row_tile * heads + it.head;
             it.part = r > 1 ? cuts0 + cut_base[lo] + pair * r + c : kWhole;
             it.pad[0] = it.pad[1] = 0;
             a.items[items0 + i] = it;
@@ -417,6 +448,226 @@ struct RowAt {  // where a tile's key and value rows are in memory
     Global v;
 };
 
+// What a lane's row sees of the new tokens: its own token and that one's
+// ancestors, found by walking up.
+struct Sight {
+    const int32_t* parents;  // the request's; null: each token's parent is the one before it
+    const int32_t* tree;     // the same in LDS, if in_lds
+    bool in_lds;
+    int32_t token;           // the row's, -1: sees none
+    int32_t at, up;          // the walk's place (-1: it has ended), and that one's parent
+
+    __device__ __forceinline__ int32_t parent_of(int32_t i) const {
+        if (in_lds) return *((const __attribute__((address_space(3))) int32_t*)tree + i);
+        return *((const __attribute__((address_space(1))) int32_t*)parents + i);
+    }
+
+    __device__ __forceinline__ void start() {
+        at = token;
+        up = at - 1;
+        if (at >= 0 && parents) {
+            up = parent_of(at);
+            if (up < -1 || up >= at) at = -1;  // void
+        }
+    }
+
+    __device__ __forceinline__ void climb() {
+        const int32_t next = up;
+        if (next < 0) {
+            at = -1;
+            return;
+        }
+        const int32_t above = parents ? parent_of(next) : next - 1;
+        at = above < -1 || above >= next ? -1 : next;
+        up = above;
+    }
+
+    // The tokens [k0, k0 + kKeys) that it sees, as bits; calls come with
+    // falling k0.
+    template <uint32_t kKeys>
+    __device__ __forceinline__ uint64_t of_tile(int32_t k0) {
+        uint64_t sees = 0;
+        if (!parents) {
+            const int32_t past = token - k0;
+            if (token >= 0 && past >= 0) sees = past >= 63 ? ~0ull : (2ull << past) - 1;
+            return kKeys == 64 ? sees : sees & 0xffffffffu;
+        }
+        while (at >= k0 + static_cast<int32_t>(kKeys)) climb();
+        while (at >= k0) {
+            sees |= 1ull << (at - k0);
+            climb();
+        }
+        return sees;
+    }
+};
+
+// A lane's place in its pair, and the tiles that the item takes.
+struct Place {
+    uint32_t token, q_head;
+    bool lives;              // the row exists
+    uint32_t part_row;       // the row's number in its row tile
+    uint32_t cached_tiles, new_tiles, first, last;
+};
+
+// Cached keys' tiles come first, then those of new tokens, from the last that
+// any of the item's rows can see to the first.
+template <uint32_t kKeys>
+__device__ __forceinline__ Place place_of(const Args& a, const Item& item, const Extent& e, uint32_t part_row) {
+    Place p;
+    const uint32_t rows = e.tokens * a.group, row0 = item.row_tile * a.row_tile_rows, row = row0 + part_row;
+    p.part_row = part_row;
+    p.lives = row < rows;
+    p.token = row / a.group;
+    p.q_head = item.head * a.group + row % a.group;
+    p.cached_tiles = ceil_div(e.cached, kKeys);
+    p.new_tiles = (min(rows, row0 + a.row_tile_rows) - 1) / a.group / kKeys + 1;
+    p.first = item.first;
+    p.last = min(item.last, p.cached_tiles + p.new_tiles);
+    return p;
+}
+
+// The item of this workgroup; false if there is none.
+__device__ __forceinline__ bool take_item(const Args& a, Item* item, Extent* e) {
+    if (a.requests <= 64) {
+        if (!item_of(a, lane_plan(a, threadIdx.x & 63u), blockIdx.x, item, e)) return false;
+    } else {
+        if (blockIdx.x >= a.head->items) return false;
+        *item = a.items[blockIdx.x];
+        *e = extent(a, item->request);
+    }
+    *item = uniform(*item);
+    *e = uniform(*e);
+    return true;
+}
+
+// Masks the scores of a tile and moves the sums' base.  Scores are s * factor;
+// where keys are masked, or the factor is negative and does not keep the
+// maximum, they are formed here, and the factor becomes one.  The base stays
+// until a score passes it by kSlack: weights are then at most 2^kSlack, which
+// every type here holds, and the accumulators are seldom scaled (l and o have
+// a common factor that the division takes out).  Returns what o is to be
+// multiplied by.
+template <uint32_t kTiles>
+__device__ __forceinline__ float new_base(f32x16* s, uint64_t sees, uint64_t full, uint32_t hi,
+                                          float* factor, float* m, float* l) {
+    if (*factor < 0.f || !__all(sees == full)) {
+#pragma unroll
+        for (uint32_t t = 0; t < kTiles; ++t) {
+            const uint32_t bits = static_cast<uint32_t>(sees >> (32 * t)) >> (4 * hi);
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i)
+                s[t][i] = (bits >> (8 * (i >> 2) + (i & 3))) & 1u ? s[t][i] * *factor : kLowest;
+        }
+        *factor = 1.f;
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (uint32_t t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64)) * *factor;
+    float grow = 1.f;
+    if (__any(top > *m + kSlack)) {
+        const float m2 = fmaxf(*m, top);
+        grow = m2 == kLowest ? 1.f : __builtin_amdgcn_exp2f(*m - m2);
+        *m = m2;
+        *l *= grow;
+    }
+    return grow;
+}
+
+// The weights of a tile's scores, as pairs of the products' type; returns
+// their sum before that rounding.
+template <class T, uint32_t kTiles>
+__device__ __forceinline__ float weights_of(const f32x16* s, float factor, float m, uint32_t (*p)[8]) {
+    const float base = m == kLowest ? 0.f : m;  // no score above the lowest yet
+    float sum = 0.f;
+#pragma unroll
+    for (uint32_t t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (uint32_t i = 0; i < 16; i += 2) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s[t][i], factor, -base));
+            const float y = __builtin_amdgcn_exp2f(fmaf(s[t][i + 1], factor, -base));
+            sum += x + y;
+            p[t][i / 2] = T::pack(x, y);
+        }
+    return sum;
+}
+
+// Writes a row, or its part.
+template <class T, uint32_t kDim, uint32_t kKeys>
+__device__ __forceinline__ void write_row(const Args& a, const Item& item, const Extent& e, const Place& p,
+                                          Sight& sight, bool odd, uint32_t hi, f32x16* o, float m, float l) {
+    if (!p.lives) return;
+    const uint32_t dim = static_cast<uint32_t>(a.cache.dim);
+    if (p.last > p.cached_tiles && odd) {
+        // Values that are not finite were left out of the products, where a
+        // weight of zero would not keep them from rows that do not see them.
+        // The rows that see them take them here (weights are above zero).
+        const uint32_t tiles = p.cached_tiles + p.new_tiles;
+        const int32_t below = static_cast<int32_t>((tiles - max(p.first, p.cached_tiles)) * kKeys);
+        const int32_t from = static_cast<int32_t>((tiles - p.last) * kKeys);
+        for (sight.start(); sight.at >= from; sight.climb()) {
+            if (sight.at >= below) continue;
+            const uint16_t* const v = static_cast<const uint16_t*>(a.v.data) +
+                                      (e.first + sight.at) * a.v.stride[0] + item.head * a.v.stride[1];
+#pragma unroll
+            for (uint32_t t = 0; t < kDim / 32; ++t)
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) {
+                    const uint32_t d = 32 * t + 8 * (i >> 2) + 4 * hi + (i & 3);
+                    const uint16_t bits = d < dim ? v[d] : 0;
+                    if ((bits & T::kExponent) == T::kExponent) o[t][i] += T::value(bits);
+                }
+        }
+    }
+    if (item.part == kWhole) {
+        bool is_void = false;
+        if (sight.parents) {
+            const int32_t up = sight.parents[p.token];
+            is_void = up < -1 || up >= static_cast<int32_t>(p.token);
+        }
+        uint16_t* const to = a.out + ((e.first + p.token) * a.q_heads + p.q_head) * dim;
+        const float inverse = 1.f / l;  // (its rounding is far below that of the result)
+#pragma unroll
+        for (uint32_t t = 0; t < kDim / 32; ++t)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; i += 4) {
+                const uint32_t d = 32 * t + 2 * i + 4 * hi;
+                if (d >= dim) continue;
+                uint2 x = make_uint2(T::pack(o[t][i] * inverse, o[t][i + 1] * inverse),
+                                     T::pack(o[t][i + 2] * inverse, o[t][i + 3] * inverse));
+                if (is_void) x = make_uint2(0, 0);
+                *reinterpret_cast<uint2*>(to + d) = x;
+            }
+    } else {
+        const uint64_t at = static_cast<uint64_t>(item.part) * a.part_rows + p.part_row;
+        float* const to = a.part_out + at * kDim;
+#pragma unroll
+        for (uint32_t t = 0; t < kDim / 32; ++t)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; i += 4)
+                *reinterpret_cast<float4*>(to + 32 * t + 2 * i + 4 * hi) =
+                    make_float4(o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]);
+        if (hi == 0) a.part_sum[at] = make_float2(m, l);
+    }
+}
+
+// Zeroes the halves of four words that are not finite; whether there were any.
+template <class T>
+__device__ __forceinline__ bool only_finite(u32x4* x) {
+    bool found = false;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t half = 0; half < 32; half += 16)
+            if ((((*x)[i] >> half) & T::kExponent) == T::kExponent) {
+                found = true;
+                (*x)[i] &= 0xffff0000u >> half;
+            }
+    return found;
+}
+
 template <class T, bool kE4M3, uint32_t kDim, uint32_t kRowWaves>
 __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_kernel(Args a) {
     using S = Shape<T, kE4M3, kDim, kRowWaves>;
@@ -431,80 +682,44 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     const uint32_t tid = threadIdx.x, lane = tid & 63u;
     Item item;
     Extent e;
-    if (a.requests <= 64) {
-        if (!item_of(a, lane_plan(a, lane), blockIdx.x, &item, &e)) return;
-    } else {
-        if (blockIdx.x >= a.head->items) return;
-        item = a.items[blockIdx.x];
-        e = extent(a, item.request);
-    }
+    if (!take_item(a, &item, &e)) return;
     const uint32_t w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const uint32_t group = w / kRowWaves, row_wave = w % kRowWaves;
     const uint32_t gtid = tid - group * S::kGroupThreads;
     const uint32_t n = lane & 31u, hi = lane >> 5;
     const uint32_t dim = static_cast<uint32_t>(a.cache.dim);
     const uint32_t page_size = static_cast<uint32_t>(a.cache.page_size);
-    const bool alike = a.cache.k_stride[0] == a.cache.v_stride[0] && a.cache.k_stride[1] == a.cache.v_stride[1];
     auto page_at = [&](uint32_t pos) { return a.page_shift < 32 ? pos >> a.page_shift : pos / page_size; };
-    const uint32_t rows = e.tokens * a.group;
-    const uint32_t row0 = item.row_tile * (kRows * kRowWaves);
-    const uint32_t row = row0 + row_wave * kRows + n;
-    const bool row_lives = row < rows;
-    const uint32_t token = row / a.group, qh = item.head * a.group + row % a.group;
+    const Place place = place_of<kKeys>(a, item, e, row_wave * kRows + n);
+    const uint32_t cached_tiles = place.cached_tiles, new_tiles = place.new_tiles;
+    const uint32_t first = place.first, last = place.last;
 
     uint8_t* const key_tile = tiles + group * 2 * S::kTileBytes;
     uint8_t* const value_tile = key_tile + S::kTileBytes;
 
-    // tiles of cached keys, then tiles of new tokens from the last that any of
-    // these rows can see to the first
-    const uint32_t cached_tiles = ceil_div(e.cached, kKeys);
-    const uint32_t last_token = (min(rows, row0 + kRows * kRowWaves) - 1) / a.group;
-    const uint32_t new_tiles = last_token / kKeys + 1;
-    const uint32_t first = item.first, last = min(item.last, cached_tiles + new_tiles);
-
-    const bool in_lds = a.parents && e.tokens <= kParentsInLds && last > cached_tiles;
-    if (in_lds)
-        for (uint32_t i = tid; i < e.tokens; i += kThreads) tree[i] = a.parents[e.first + i];
+    Sight sight;
+    sight.parents = a.parents ? a.parents + e.first : nullptr;
+    sight.tree = tree;
+    sight.in_lds = a.parents && e.tokens <= kParentsInLds && last > cached_tiles;
+    sight.token = place.lives && last > cached_tiles ? static_cast<int32_t>(place.token) : -1;
+    if (sight.in_lds)
+        for (uint32_t i = tid; i < e.tokens; i += kThreads) tree[i] = sight.parents[i];
     if (tid == 0) odd = 0;
     // the rows' queries, permuted as the keys are
     uint8_t* const query_tile = queries + row_wave * kRows * kDim * 2;
     if (group == 0) {
         const uint16_t* const base = static_cast<const uint16_t*>(a.q.data) +
-                                     (e.first + token) * a.q.stride[0] + qh * a.q.stride[1];
+                                     (e.first + place.token) * a.q.stride[0] + place.q_head * a.q.stride[1];
 #pragma unroll
         for (uint32_t c = 0; c < kDim / 16; ++c) {
             const uint32_t d = 16 * c + 8 * hi;
             u32x4 x = {0, 0, 0, 0};
-            if (row_lives && d < dim) x = *reinterpret_cast<const u32x4*>(base + d);
+            if (place.lives && d < dim) x = *reinterpret_cast<const u32x4*>(base + d);
             *reinterpret_cast<u32x4*>(query_tile + (n * S::kChunks + key_chunk<kDim>(n, 2 * c + hi)) * 16) = x;
         }
     }
     __syncthreads();  // (all groups read the queries, which the first one writes)
-    const int32_t* const parents = a.parents ? a.parents + e.first : nullptr;
-    auto parent_of = [&](int32_t i) { return in_lds ? tree[i] : parents[i]; };
-
-    // the row's place on its way up: a token that it sees (-1: none is left),
-    // and that one's parent
-    int32_t at = -1, up = -1;
-    auto start = [&]() {
-        at = row_lives && last > cached_tiles ? static_cast<int32_t>(token) : -1;
-        up = at - 1;
-        if (at >= 0 && parents) {
-            up = parent_of(at);
-            if (up < -1 || up >= at) at = -1;
-        }
-    };
-    auto climb = [&]() {
-        const int32_t next = up;
-        if (next < 0) {
-            at = -1;
-            return;
-        }
-        const int32_t above = parents ? parent_of(next) : next - 1;
-        at = above < -1 || above >= next ? -1 : next;
-        up = above;
-    };
-    start();
+    sight.start();
 
     f32x16 o[S::kDTiles];
 #pragma unroll
@@ -539,10 +754,15 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
             const uint32_t pos = tile * kKeys + my_key;
             counts = pos < e.cached && static_cast<uint32_t>(page) < a.cache.num_pages;
             if (counts) {
-                const uint64_t place = pos - page_at(pos) * page_size, p = static_cast<uint32_t>(page);
-                const uint64_t at_k = (p * a.cache.k_stride[0] + place * a.cache.k_stride[1]) * size;
-                r.k = ck + at_k;
-                r.v = cv + (alike ? at_k : (p * a.cache.v_stride[0] + place * a.cache.v_stride[1]) * size);
+                const uint32_t in_page = pos - page_at(pos) * page_size, p = static_cast<uint32_t>(page);
+                if (a.narrow) {
+                    const uint64_t at = static_cast<uint64_t>(p) * a.page_bytes + in_page * a.place_bytes;
+                    r.k = ck + at;
+                    r.v = cv + at;
+                } else {
+                    r.k = ck + (p * a.cache.k_stride[0] + in_page * a.cache.k_stride[1]) * size;
+                    r.v = cv + (p * a.cache.v_stride[0] + in_page * a.cache.v_stride[1]) * size;
+                }
             }
         } else {
             const uint32_t j = (cached_tiles + new_tiles - 1 - tile) * kKeys + my_key;
@@ -607,21 +827,14 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
                 put(r, 2 * chunk8 + 1, k2[1], v2[1]);
             }
         } else {
-            uint32_t found = 0;
+            bool found = false;
 #pragma unroll
             for (uint32_t j = 0; j < kLoads; ++j) {
                 const uint32_t r = row_of_load + j * kRowStep;
                 u32x4 kx = kreg[j], vx = vreg[j];
                 if (!whole && !(((counts >> r) & 1u) && chunk * 8 < dim)) kx = vx = zero;
                 if (tile >= cached_tiles)
-#pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-                        for (uint32_t half = 0; half < 32; half += 16)
-                            if (((vx[i] >> half) & T::kExponent) == T::kExponent) {
-                                found = 1;
-                                vx[i] &= 0xffff0000u >> half;
-                            }
+                    found |= only_finite<T>(&vx);
                 put(r, chunk, kx, vx);
             }
             if (found) odd = 1;
@@ -675,64 +888,12 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
             }
             // which keys this lane's row sees
             uint64_t sees = counts;
-            if (is_new) {
-                const int32_t k0 = static_cast<int32_t>((cached_tiles + new_tiles - 1 - tile) * kKeys);
-                sees = 0;
-                if (!parents) {
-                    const int32_t past = static_cast<int32_t>(token) - k0;
-                    if (row_lives && past >= 0) sees = past >= 63 ? ~0ull : (2ull << past) - 1;
-                    sees &= kFull;
-                } else {
-                    while (at >= k0 + static_cast<int32_t>(kKeys)) climb();
-                    while (at >= k0) {
-                        sees |= 1ull << (at - k0);
-                        climb();
-                    }
-                }
-            }
-            // scores are s * factor; where keys are masked, or the factor is
-            // negative and does not keep the maximum, they are formed first
+            if (is_new)
+                sees = sight.of_tile<kKeys>(static_cast<int32_t>((cached_tiles + new_tiles - 1 - tile) * kKeys));
             float factor = is_new ? new_scale : cached_scale;
-            if (factor < 0.f || !__all(sees == kFull)) {
-#pragma unroll
-                for (uint32_t t = 0; t < S::kSTiles; ++t) {
-                    const uint32_t bits = static_cast<uint32_t>(sees >> (32 * t)) >> (4 * hi);
-#pragma unroll
-                    for (uint32_t i = 0; i < 16; ++i)
-                        s[t][i] = (bits >> (8 * (i >> 2) + (i & 3))) & 1u ? s[t][i] * factor : kLowest;
-                }
-                factor = 1.f;
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (uint32_t t = 0; t < S::kSTiles; ++t)
-#pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-            top = fmaxf(top, __shfl_xor(top, 32, 64)) * factor;
-            // The sums keep their base until a score passes it by kSlack: weights
-            // are then at most 2^kSlack, which every type here holds, and the
-            // accumulators are seldom scaled (m below the base's row maximum
-            // by less than that only moves the common factor of l and o).
-            float grow = 1.f;
-            if (__any(top > m + kSlack)) {
-                const float m2 = fmaxf(m, top);
-                grow = m2 == kLowest ? 1.f : __builtin_amdgcn_exp2f(m - m2);
-                m = m2;
-                l *= grow;
-            }
-            const float base = m == kLowest ? 0.f : m;  // no score above the lowest yet
-            float sum = 0.f;
+            float grow = new_base<S::kSTiles>(s, sees, kFull, hi, &factor, &m, &l);
             uint32_t p[S::kSTiles][8];
-#pragma unroll
-            for (uint32_t t = 0; t < S::kSTiles; ++t)
-#pragma unroll
-                for (uint32_t i = 0; i < 16; i += 2) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[t][i], factor, -base));
-                    const float y = __builtin_amdgcn_exp2f(fmaf(s[t][i + 1], factor, -base));
-                    sum += x + y;
-                    p[t][i / 2] = T::pack(x, y);
-                }
-            l += sum;
+            l += weights_of<T, S::kSTiles>(s, factor, m, p);
             if (kE4M3 && is_new && !scaled) {
                 grow *= value_scale;
                 scaled = true;
@@ -775,12 +936,6 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i) o[t][i] *= value_scale;
 
-    const bool is_whole = item.part == kWhole;
-    bool is_void = false;
-    if (parents && row_lives) {
-        const int32_t p = parents[token];
-        is_void = p < -1 || p >= static_cast<int32_t>(token);
-    }
     if constexpr (S::kGroups > 1) {
         // join the groups: each scales its part to the common maximum and adds
         // it to the first one's, a group after the other
@@ -819,51 +974,352 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
         m = m_all;
         l = l_all;
     }
-    if (!row_lives) return;
-    if (last > cached_tiles && odd) {
-        // Values that are not finite were left out above, where a weight of
-        // zero would not keep them from rows that do not see them.  The rows
-        // that see them take them here (weights are above zero).
-        const int32_t below = static_cast<int32_t>((cached_tiles + new_tiles - max(first, cached_tiles)) * kKeys);
-        const int32_t from = static_cast<int32_t>((cached_tiles + new_tiles - last) * kKeys);
-        for (start(); at >= from; climb()) {
-            if (at >= below) continue;
-            const uint16_t* const v = static_cast<const uint16_t*>(a.v.data) +
-                                      (e.first + at) * a.v.stride[0] + item.head * a.v.stride[1];
+    write_row<T, kDim, kKeys>(a, item, e, place, sight, odd, hi, o, m, l);
+}
+
+// ---------------------------------------------------------------------------
+// The attention kernel for many rows
+// ---------------------------------------------------------------------------
+
+// Four wavefronts share every tile, 32 rows each, and the matrix instructions
+// bound the work.  Tiles are brought to LDS without passing through registers,
+// in two buffers each for keys and values; a wavefront brings a quarter of
+// each tile, and one barrier a tile remains.  Operands are read from LDS a few
+// products ahead (the compiler alone reads each where it is needed, and every
+// product then waits for LDS).  8-bit tiles stay 8-bit in LDS and become
+// operands as they are read.
+template <bool kE4M3, uint32_t kDim>
+struct Wide {
+    static constexpr uint32_t kKeys = kDim == 256 ? 32 : 64;
+    static constexpr uint32_t kChunks = kDim / 8;     // 16-byte chunks of a 16-bit row
+    static constexpr uint32_t kChunks8 = kDim / 16;   // and of an 8-bit row
+    static constexpr uint32_t kOwnRows = kKeys / 4;   // rows that a wavefront brings
+    static constexpr uint32_t kLoads = kOwnRows * kChunks / 64, kLoads8 = kOwnRows * kChunks8 / 64;
+    static constexpr uint32_t kTileBytes = kKeys * kDim * 2;
+    static constexpr uint32_t kSTiles = kKeys / 32, kDTiles = kDim / 32;
+    static_assert(kLoads >= 1 && kLoads8 >= 1, "every wavefront brings something");
+};
+
+// Where chunk c of an 8-bit row r lies in its row.
+template <uint32_t kDim>
+__device__ __forceinline__ uint32_t chunk_of_8(uint32_t r, uint32_t c) {
+    return kDim == 64 ? c ^ ((r >> 2) & 3u) : kDim == 128 ? c ^ ((r >> 1) & 7u) : c ^ (r & 15u);
+}
+
+// What is read in place of rows that do not count.
+__device__ uint4 zero_row[kRows];
+static_assert(sizeof(zero_row) >= 2 * coop_pages::kMaxDim, "a row of zeros");
+
+// Products in order, each one's operand read from LDS kAhead products before
+// it; no read or product moves across another step.
+constexpr uint32_t kAhead = 4;
+
+template <uint32_t kProducts, class Read, class Multiply>
+__device__ __forceinline__ void products(Read read, Multiply multiply) {
+    u32x4 x[kAhead];
 #pragma unroll
-            for (uint32_t t = 0; t < S::kDTiles; ++t)
+    for (uint32_t i = 0; i < kAhead; ++i) x[i] = read(i);
 #pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) {
-                    const uint32_t d = 32 * t + 8 * (i >> 2) + 4 * hi + (i & 3);
-                    const uint16_t bits = d < dim ? v[d] : 0;
-                    if ((bits & T::kExponent) == T::kExponent) o[t][i] += T::value(bits);
+    for (uint32_t i = 0; i < kProducts; ++i) {
+        __builtin_amdgcn_sched_barrier(0x6);  // (scalar and vector arithmetic may move)
+        multiply(i, x[i % kAhead]);
+        if (i + kAhead < kProducts) x[i % kAhead] = read(i + kAhead);
+    }
+    __builtin_amdgcn_sched_barrier(0x6);
+}
+
+struct Eight { static constexpr bool value = true; };   // bits of a tile's numbers
+struct Sixteen { static constexpr bool value = false; };
+
+template <class T, bool kE4M3, uint32_t kDim>
+__global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_wide_kernel(Args a) {
+    using W = Wide<kE4M3, kDim>;
+    constexpr uint32_t kKeys = W::kKeys;
+    constexpr uint64_t kFull = kKeys == 64 ? ~0ull : 0xffffffffull;
+    __shared__ __align__(16) uint8_t keys0[W::kTileBytes], keys1[W::kTileBytes];
+    __shared__ __align__(16) uint8_t values0[W::kTileBytes], values1[W::kTileBytes];
+    __shared__ int32_t tree[kParentsInLds];
+    __shared__ uint32_t odd;
+
+    const uint32_t tid = threadIdx.x, lane = tid & 63u;
+    Item item;
+    Extent e;
+    if (!take_item(a, &item, &e)) return;
+    const uint32_t w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const uint32_t n = lane & 31u, hi = lane >> 5;
+    const uint32_t dim = static_cast<uint32_t>(a.cache.dim);
+    const uint32_t page_size = static_cast<uint32_t>(a.cache.page_size);
+    auto page_at = [&](uint32_t pos) { return a.page_shift < 32 ? pos >> a.page_shift : pos / page_size; };
+    const Place place = place_of<kKeys>(a, item, e, w * kRows + n);
+    const uint32_t cached_tiles = place.cached_tiles, all_tiles = place.cached_tiles + place.new_tiles;
+    const uint32_t first = place.first, last = place.last;
+
+    const uint64_t size = kE4M3 ? 1 : 2;
+    const Global ck = (Global)(a.cache.k) + item.head * a.cache.k_stride[2] * size;
+    const Global cv = (Global)(a.cache.v) + item.head * a.cache.v_stride[2] * size;
+    const Global nk = (Global)(a.k.data) + (e.first * a.k.stride[0] + item.head * a.k.stride[1]) * 2;
+    const Global nv = (Global)(a.v.data) + (e.first * a.v.stride[0] + item.head * a.v.stride[1]) * 2;
+    const Global zeros = (Global)(&zero_row[0]);
+
+    // A lane knows where the rows of the tile's key lane % kKeys are, as offsets
+    // from the tile's base; kNowhere: a row that does not count.
+    constexpr uint64_t kNowhere = ~0ull;
+    const uint32_t my_key = lane % kKeys;
+    const uint32_t table_end = min(cached_tiles, last) * kKeys < e.cached ? min(cached_tiles, last) * kKeys : e.cached;
+    const int32_t* const table = a.table + static_cast<uint64_t>(item.request) * a.max_pages;
+    auto page_of = [&](uint32_t tile) -> int32_t {
+        const uint32_t pos = tile * kKeys + my_key;
+        return pos < table_end ? table[page_at(pos)] : -1;
+    };
+    struct Where {
+        uint64_t k, v;
+        uint64_t counts;  // which of the tile's keys count
+    };
+    auto locate = [&](uint32_t tile, int32_t page) {
+        Where r = {kNowhere, kNowhere, 0};
+        if (tile < cached_tiles) {
+            const uint32_t pos = tile * kKeys + my_key;
+            if (static_cast<uint32_t>(page) < static_cast<uint32_t>(a.cache.num_pages)) {
+                const uint32_t in_page = pos - page_at(pos) * page_size, p = static_cast<uint32_t>(page);
+                if (a.narrow) {
+                    r.k = static_cast<uint64_t>(p) * a.page_bytes + in_page * a.place_bytes;
+                    r.v = r.k;
+                } else {
+                    r.k = (p * a.cache.k_stride[0] + in_page * a.cache.k_stride[1]) * size;
+                    r.v = (p * a.cache.v_stride[0] + in_page * a.cache.v_stride[1]) * size;
                 }
+            }
+        } else {
+            const uint32_t j = (all_tiles - 1 - tile) * kKeys + my_key;
+            if (tile < last && j < e.tokens) {
+                r.k = j * a.k.stride[0] * 2;
+                r.v = j * a.v.stride[0] * 2;
+            }
+        }
+        const uint64_t all = __ballot(r.k != kNowhere);
+        r.counts = kKeys == 64 ? all : all & 0xffffffffu;
+        return r;
+    };
+    auto from = [&](uint64_t v, uint32_t r) -> uint64_t {
+        return static_cast<uint64_t>(__shfl(static_cast<uint32_t>(v), r, 64)) |
+               static_cast<uint64_t>(__shfl(static_cast<uint32_t>(v >> 32), r, 64)) << 32;
+    };
+    auto fetch = [](Global p, uint8_t* to) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                         (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    };
+    // Brings this wavefront's rows of a tile: lane by lane to consecutive
+    // chunks of LDS, so each lane fetches the chunk whose place that is.
+    auto bring = [&](uint32_t tile, const Where& at, uint8_t* keys, uint8_t* values) {
+        if (tile >= last) return;
+        const bool cached = tile < cached_tiles, same = cached && a.narrow;
+        const bool plain = dim == kDim && at.counts == kFull;  // nothing is zeroed
+        auto rows_of = [&](uint32_t r, Global kb, Global vb, Global* k, Global* v) {
+            const uint64_t ok = from(at.k, r), ov = same ? ok : from(at.v, r);
+            *k = kb + ok;
+            *v = vb + ov;
+            if (!plain && ok == kNowhere) *k = *v = zeros;
+        };
+        if (kE4M3 && cached) {
+#pragma unroll
+            for (uint32_t j = 0; j < W::kLoads8; ++j) {
+                const uint32_t slot = j * 64 + lane, r = w * W::kOwnRows + slot / W::kChunks8;
+                const uint32_t c = chunk_of_8<kDim>(r, slot % W::kChunks8) * 16;
+                const uint32_t to = (w * W::kOwnRows * W::kChunks8 + j * 64) * 16;
+                Global k, v;
+                rows_of(r, ck, cv, &k, &v);
+                fetch(plain || c < dim ? k + c : zeros, keys + to);
+                fetch(plain || c < dim ? v + c : zeros, values + to);
+            }
+        } else {
+            const Global kb = cached ? ck : nk, vb = cached ? cv : nv;
+#pragma unroll
+            for (uint32_t j = 0; j < W::kLoads; ++j) {
+                const uint32_t slot = j * 64 + lane, r = w * W::kOwnRows + slot / W::kChunks;
+                const uint32_t ks = key_chunk<kDim>(r, slot % W::kChunks) * 16;
+                const uint32_t vs = value_chunk<kDim>(r, slot % W::kChunks) * 16;
+                const uint32_t to = (w * W::kOwnRows * W::kChunks + j * 64) * 16;
+                Global k, v;
+                rows_of(r, kb, vb, &k, &v);
+                fetch(plain || ks < 2 * dim ? k + ks : zeros, keys + to);
+                fetch(plain || vs < 2 * dim ? v + vs : zeros, values + to);
+            }
+        }
+    };
+    // Takes out of this wavefront's rows of new values what is not finite.
+    auto clean = [&](uint8_t* values) {
+#pragma unroll
+        for (uint32_t j = 0; j < W::kLoads; ++j) {
+            u32x4* const p = reinterpret_cast<u32x4*>(values) + w * W::kOwnRows * W::kChunks + j * 64 + lane;
+            u32x4 x = *p;
+            if (only_finite<T>(&x)) {
+                *p = x;
+                odd = 1;
+            }
+        }
+    };
+    auto arrived = [&]() {
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): what this wavefront brings is there
+        asm volatile("" ::: "memory");
+    };
+
+    // the first tile's rows are on their way before anything else is
+    const int32_t first_page = page_of(first), second_page = page_of(first + 1);
+    int32_t page = page_of(first + 2);
+    Where now = locate(first, first_page);  // of the tile that is next
+    bring(first, now, keys0, values0);
+
+    Sight sight;
+    sight.parents = a.parents ? a.parents + e.first : nullptr;
+    sight.tree = tree;
+    sight.in_lds = a.parents && e.tokens <= kParentsInLds && last > cached_tiles;
+    sight.token = place.lives && last > cached_tiles ? static_cast<int32_t>(place.token) : -1;
+    if (sight.in_lds)
+        for (uint32_t i = tid; i < e.tokens; i += kThreads) tree[i] = sight.parents[i];
+    if (tid == 0) odd = 0;
+    u32x4 q[kDim / 16];
+    {
+        const uint16_t* const base = static_cast<const uint16_t*>(a.q.data) +
+                                     (e.first + place.token) * a.q.stride[0] + place.q_head * a.q.stride[1];
+#pragma unroll
+        for (uint32_t c = 0; c < kDim / 16; ++c) {
+            const uint32_t d = 16 * c + 8 * hi;
+            q[c] = u32x4{0, 0, 0, 0};
+            if (place.lives && d < dim) q[c] = *reinterpret_cast<const u32x4*>(base + d);
         }
     }
-    if (is_whole) {
-        uint16_t* const to = a.out + ((e.first + token) * a.q_heads + qh) * dim;
+    Where next = locate(first + 1, second_page);
+    f32x16 o[W::kDTiles];
 #pragma unroll
-        for (uint32_t t = 0; t < S::kDTiles; ++t)
+    for (uint32_t t = 0; t < W::kDTiles; ++t)
 #pragma unroll
-            for (uint32_t i = 0; i < 16; i += 4) {
-                const uint32_t d = 32 * t + 2 * i + 4 * hi;
-                if (d >= dim) continue;
-                uint2 x = make_uint2(T::pack(o[t][i] / l, o[t][i + 1] / l),
-                                     T::pack(o[t][i + 2] / l, o[t][i + 3] / l));
-                if (is_void) x = make_uint2(0, 0);
-                *reinterpret_cast<uint2*>(to + d) = x;
-            }
-    } else {
-        const uint64_t at_row = static_cast<uint64_t>(item.part) * a.part_rows + row_wave * kRows + n;
-        float* const to = a.part_out + at_row * kDim;
+        for (uint32_t i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m = kLowest, l = 0.f;
+    const float new_scale = a.scale * kLog2e;
+    const float cached_scale = kE4M3 ? new_scale * a.cache.k_scale[item.head] : new_scale;
+    const float value_scale = kE4M3 ? a.cache.v_scale[item.head] : 1.f;
+    bool scaled = false;  // whether o has met the cached values' scale
+
+    // an operand as it is read, and as products take it
+    auto operand = [](u32x4 x, auto width) -> u32x4 {
+        if constexpr (decltype(width)::value)
+            return {T::template from_e4m3<false>(x[0]), T::template from_e4m3<true>(x[0]),
+                    T::template from_e4m3<false>(x[1]), T::template from_e4m3<true>(x[1])};
+        else
+            return x;
+    };
+    // the products of a tile's keys with the rows' queries
+    auto scores = [&](const uint8_t* __restrict__ keys, f32x16* to, auto width) {
 #pragma unroll
-        for (uint32_t t = 0; t < S::kDTiles; ++t)
+        for (uint32_t t = 0; t < W::kSTiles; ++t)
 #pragma unroll
-            for (uint32_t i = 0; i < 16; i += 4)
-                *reinterpret_cast<float4*>(to + 32 * t + 2 * i + 4 * hi) =
-                    make_float4(o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]);
-        if (hi == 0) a.part_sum[at_row] = make_float2(m, l);
+            for (uint32_t i = 0; i < 16; ++i) to[t][i] = 0.f;
+        products<kDim / 16 * W::kSTiles>(
+            [&](uint32_t i) -> u32x4 {
+                const uint32_t c = i / W::kSTiles, r = 32 * (i % W::kSTiles) + n;
+                if constexpr (decltype(width)::value) {
+                    const uint2 x = *reinterpret_cast<const uint2*>(
+                        keys + (r * W::kChunks8 + chunk_of_8<kDim>(r, c)) * 16 + hi * 8);
+                    return {x.x, x.y, 0, 0};
+                } else {
+                    return *reinterpret_cast<const u32x4*>(
+                        keys + (r * W::kChunks + key_chunk<kDim>(r, 2 * c + hi)) * 16);
+                }
+            },
+            [&](uint32_t i, u32x4 x) {
+                const uint32_t t = i % W::kSTiles;
+                to[t] = T::mfma(operand(x, width), q[i / W::kSTiles], to[t]);
+            });
+    };
+    // adds a tile's values by their weights
+    auto add = [&](const uint8_t* __restrict__ values, uint32_t (*p)[8], auto width) {
+        const uint32_t g = lane & 15u;
+        products<2 * W::kSTiles * W::kDTiles>(
+            [&](uint32_t i) -> u32x4 {
+                const uint32_t dt = i % W::kDTiles, r0 = 16 * (i / W::kDTiles) + 4 * hi;
+                if constexpr (decltype(width)::value) {
+                    // eight rows of 16 columns: keys 0..3 and 8..11 of the lane's half
+                    typedef int i32x2 __attribute__((ext_vector_type(2)));
+                    typedef __attribute__((address_space(3))) i32x2 Two;
+                    const uint32_t r = r0 + ((g >> 1) & 3u) + (g & 8u), c = 2 * dt + ((lane >> 4) & 1u);
+                    const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                        (Two*)(values + (r * W::kChunks8 + chunk_of_8<kDim>(r, c)) * 16 + (g & 1u) * 8));
+                    return {static_cast<uint32_t>(x[0]), static_cast<uint32_t>(x[1]), 0, 0};
+                } else {
+                    typedef __attribute__((address_space(3))) s16x4 Four;
+                    const uint32_t r = r0 + (g >> 2), d = 32 * dt + (lane & 16u) + 4 * (g & 3u);
+                    const uint8_t* const at = values + (r * W::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2;
+                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four*)at);
+                    // (rows eight apart are permuted alike)
+                    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four*)(at + 8 * kDim * 2));
+                    const uint2 a0 = __builtin_bit_cast(uint2, v0), a1 = __builtin_bit_cast(uint2, v1);
+                    return {a0.x, a0.y, a1.x, a1.y};
+                }
+            },
+            [&](uint32_t i, u32x4 x) {
+                const uint32_t dt = i % W::kDTiles, t = i / W::kDTiles / 2, half = i / W::kDTiles % 2;
+                const u32x4 px = {p[t][4 * half], p[t][4 * half + 1], p[t][4 * half + 2], p[t][4 * half + 3]};
+                o[dt] = T::mfma(operand(x, width), px, o[dt]);
+            });
+    };
+    // A tile, on its way to `keys` and `values`.
+    auto step = [&](uint32_t tile, auto width, uint8_t* __restrict__ keys, uint8_t* __restrict__ values,
+                    uint8_t* __restrict__ keys_to, uint8_t* __restrict__ values_to) {
+        constexpr bool kNew = kE4M3 && !decltype(width)::value;  // (a 16-bit tile of an 8-bit cache's call)
+        const bool is_new = kNew || tile >= cached_tiles;
+        arrived();
+        if (is_new) clean(values);
+        __syncthreads();
+        const uint64_t counts = now.counts;
+        bring(tile + 1, next, keys_to, values_to);
+        now = next;
+        next = locate(tile + 2, page);
+        page = page_of(tile + 3);
+
+        f32x16 s[W::kSTiles];
+        scores(keys, s, width);
+        uint64_t sees = counts;
+        if (is_new) sees = sight.of_tile<kKeys>(static_cast<int32_t>((all_tiles - 1 - tile) * kKeys));
+        float factor = is_new ? new_scale : cached_scale;
+        float grow = new_base<W::kSTiles>(s, sees, kFull, hi, &factor, &m, &l);
+        if (kNew && !scaled) {
+            grow *= value_scale;
+            scaled = true;
+        }
+        if (!__all(grow == 1.f))
+#pragma unroll
+            for (uint32_t t = 0; t < W::kDTiles; ++t)
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) o[t][i] *= grow;
+        uint32_t p[W::kSTiles][8];
+        l += weights_of<T, W::kSTiles>(s, factor, m, p);
+        add(values, p, width);
+    };
+    __syncthreads();  // (the tree, and that no value is odd yet)
+    sight.start();
+    uint32_t tile = first;
+    if constexpr (kE4M3) {
+        const uint32_t end = min(last, cached_tiles);
+        for (; tile + 1 < end; tile += 2) {
+            step(tile, Eight(), keys0, values0, keys1, values1);
+            step(tile + 1, Eight(), keys1, values1, keys0, values0);
+        }
+        if (tile < end) {  // (an odd number: the buffers' parts are exchanged)
+            step(tile++, Eight(), keys0, values0, keys1, values1);
+            if (tile < last) step(tile++, Sixteen(), keys1, values1, keys0, values0);
+        }
     }
+    for (; tile < last; tile += 2) {
+        step(tile, Sixteen(), keys0, values0, keys1, values1);
+        if (tile + 1 < last) step(tile + 1, Sixteen(), keys1, values1, keys0, values0);
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (kE4M3 && !scaled)
+#pragma unroll
+        for (uint32_t t = 0; t < W::kDTiles; ++t)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) o[t][i] *= value_scale;
+    write_row<T, kDim, kKeys>(a, item, e, place, sight, odd, hi, o, m, l);
 }
 
 // Joins the parts of rows whose keys were cut.  A row's parts are dealt to
@@ -976,7 +1432,7 @@ Plan plan_of(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t head
     // wavefronts along the rows: as many as an average request fills
     const uint64_t mean = requests ? (rows + requests - 1) / requests : 0;
     p.row_waves = mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
-    p.tile_keys = p.row_waves == 4 ? 64 : 32;
+    p.tile_keys = p.row_waves == 4 && p.dim != 256 ? 64 : 32;
     p.target = 1024;
     const uint64_t tile_rows = kRows * p.row_waves;
     p.part_rows = static_cast<uint32_t>(rows < tile_rows ? rows : tile_rows);
@@ -995,7 +1451,7 @@ template <class T, bool kE4M3, uint32_t kDim>
 void launch(const Plan& p, const Args& a, uint32_t joins, hipStream_t s) {
     auto kernel = p.row_waves == 1   ? tree_attention_kernel<T, kE4M3, kDim, 1>
                   : p.row_waves == 2 ? tree_attention_kernel<T, kE4M3, kDim, 2>
-                                     : tree_attention_kernel<T, kE4M3, kDim, 4>;
+                                     : tree_attention_wide_kernel<T, kE4M3, kDim>;
     hipLaunchKernelGGL(kernel, dim3(a.max_items), dim3(kThreads), 0, s, a);
     if (joins) {
         // the rows of all pairs: fewer than the device has wavefronts, or more
@@ -1065,6 +1521,12 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     a.group = static_cast<uint32_t>(q_heads / cache->heads);
     a.page_shift = (cache->page_size & (cache->page_size - 1)) == 0
                        ? static_cast<uint32_t>(__builtin_ctzll(cache->page_size)) : 32u;
+    const uint64_t size = cache->type == COOP_E4M3 ? 1 : 2;
+    a.narrow = cache->k_stride[0] == cache->v_stride[0] && cache->k_stride[1] == cache->v_stride[1] &&
+               cache->k_stride[0] * size < 1ull << 32 && cache->k_stride[1] * size < 1ull << 32 &&
+               cache->k_stride[1] * size * cache->page_size < 1ull << 32;
+    a.page_bytes = static_cast<uint32_t>(cache->k_stride[0] * size);
+    a.place_bytes = static_cast<uint32_t>(cache->k_stride[1] * size);
     a.scale = scale;
     a.tile_keys = p.tile_keys;
     a.row_tile_rows = kRows * p.row_waves;
