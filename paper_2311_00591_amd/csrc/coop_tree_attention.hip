@@ -88,7 +88,7 @@ struct Args {
     uint32_t page_bytes, place_bytes;
     float scale;
     // the plan and the workspace
-    uint32_t tile_keys, row_tile_rows, target, least, chunk_multiple, max_items, part_rows;
+    uint32_t tile_keys, row_tile_rows, slots, least, chunk_multiple, max_items, part_rows;
     Head* head;
     Item* items;
     Join* joins;
@@ -118,17 +118,55 @@ __device__ __forceinline__ Extent extent(const Args& a, uint32_t b) {
 
 __device__ __forceinline__ uint32_t ceil_div(uint32_t x, uint32_t y) { return (x + y - 1) / y; }
 
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
-    for (uint32_t d = 32; d; d >>= 1) v += __shfl_xor(v, d, 64);
-    return v;
+// v of the lane that a step of a scan adds: one, two, four, eight lanes below in
+// rows of 16, then the last lane of the row before, then lane 31; 0 where there
+// is none.
+template <int kStep>
+__device__ __forceinline__ uint32_t from_below(uint32_t v) {
+    constexpr int kControl = kStep < 4 ? 0x110 + (1 << kStep) : kStep == 4 ? 0x142 : 0x143;
+    constexpr int kRowMask = kStep < 4 ? 0xf : kStep == 4 ? 0xa : 0xc;
+    return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), kControl, kRowMask, 0xf, false));
 }
 
-// All ranges are `chunk` tiles long, a length that gives about `target` of them
-// when the keys are spread evenly: with W tiles in all, chunk >= W / target, so
-// the rows that are cut make at most 2 target parts.
-__device__ __forceinline__ uint32_t chunk_of(const Args& a, uint64_t work) {
-    const double even = ceil(static_cast<double>(work) / a.target);
-    const uint32_t n = even < 0x1p30 ? max(static_cast<uint32_t>(even), a.least) : 1u << 30;
+template <int kStep>
+__device__ __forceinline__ uint64_t from_below(uint64_t v) {
+    return from_below<kStep>(static_cast<uint32_t>(v)) |
+           static_cast<uint64_t>(from_below<kStep>(static_cast<uint32_t>(v >> 32))) << 32;
+}
+
+// Running sums over a wavefront's lanes.
+template <class U>
+__device__ __forceinline__ U scan_lanes(U v) {
+    v += from_below<0>(v);
+    v += from_below<1>(v);
+    v += from_below<2>(v);
+    v += from_below<3>(v);
+    v += from_below<4>(v);
+    return v + from_below<5>(v);
+}
+
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, uint32_t lane) {
+    return __builtin_amdgcn_readlane(v, lane);
+}
+__device__ __forceinline__ uint64_t from_lane(uint64_t v, uint32_t lane) {
+    return from_lane(static_cast<uint32_t>(v), lane) |
+           static_cast<uint64_t>(from_lane(static_cast<uint32_t>(v >> 32), lane)) << 32;
+}
+
+template <class U>
+__device__ __forceinline__ U wave_sum(U v) { return from_lane(scan_lanes(v), 63); }
+
+// Pairs (a request's row tile and head) of many tiles are cut into ranges of
+// `chunk` tiles, all of one length.  Workgroups take ranges as they come free,
+// a.slots of them at once.  If ranges that cut the whole work evenly among the
+// slots all fit at once, they end together; where pairs leave too many
+// remainders for that, ranges of half the length keep the wait for the last
+// ones short.  Shorter ones yet cost more in starts, ends and joins than they
+// save (and this plan, which every wavefront makes, has to be short itself).
+// Ranges no shorter than W / n tiles, W the whole work, leave at most 2 n parts.
+__device__ __forceinline__ uint32_t chunk_of(const Args& a, uint64_t work, uint32_t slots) {
+    const float even = ceilf(static_cast<float>(work) / static_cast<float>(slots)) + 1.f;
+    const uint32_t n = even < 0x1p30f ? max(static_cast<uint32_t>(even), a.least) : 1u << 30;
     return (n + a.chunk_multiple - 1) / a.chunk_multiple * a.chunk_multiple;
 }
 
@@ -137,15 +175,7 @@ __device__ __forceinline__ uint32_t row_tiles_of(const Args& a, uint32_t tokens)
 }
 
 __device__ __forceinline__ uint32_t tiles_of(const Args& a, const Extent& e) {
-    return ceil_div(e.cached, a.tile_keys) + ceil_div(e.tokens, a.tile_keys);
-}
-
-__device__ __forceinline__ uint32_t scan_lanes(uint32_t v, uint32_t lane) {
-    for (uint32_t d = 1; d < 64; d <<= 1) {
-        const uint32_t up = __shfl_up(v, d, 64);
-        if (lane >= d) v += up;
-    }
-    return v;
+    return e.tokens ? ceil_div(e.cached, a.tile_keys) + ceil_div(e.tokens, a.tile_keys) : 0;
 }
 
 // The plan of at most 64 requests, which every wavefront makes for itself: a
@@ -161,19 +191,17 @@ __device__ __forceinline__ LanePlan lane_plan(const Args& a, uint32_t lane) {
     p.e = Extent{0, 0, 0};
     if (lane < a.requests) p.e = extent(a, lane);
     const uint32_t heads = static_cast<uint32_t>(a.cache.heads);
-    p.tiles = p.e.tokens ? tiles_of(a, p.e) : 0;
+    p.tiles = tiles_of(a, p.e);
     p.pairs = row_tiles_of(a, p.e.tokens) * heads;
-    p.chunk = chunk_of(a, wave_sum(static_cast<uint64_t>(p.pairs) * p.tiles));
+    const uint64_t work = wave_sum(static_cast<uint64_t>(p.pairs) * p.tiles);
+    p.chunk = chunk_of(a, work, a.slots);
+    if (wave_sum(p.pairs * ceil_div(p.tiles, p.chunk)) > a.slots) p.chunk = chunk_of(a, work, 2 * a.slots);
     p.ranges = ceil_div(p.tiles, p.chunk);
     const bool cut = p.ranges > 1;
-    p.items = scan_lanes(p.pairs * p.ranges, lane);
-    p.cuts = scan_lanes(cut ? p.pairs * p.ranges : 0, lane);
-    p.joins = scan_lanes(cut ? p.pairs : 0, lane);
+    p.items = scan_lanes(p.pairs * p.ranges);
+    p.cuts = scan_lanes(cut ? p.pairs * p.ranges : 0u);
+    p.joins = scan_lanes(cut ? p.pairs : 0u);
     return p;
-}
-
-__device__ __forceinline__ uint32_t from_lane(uint32_t v, uint32_t lane) {
-    return __builtin_amdgcn_readlane(v, lane);
 }
 
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -250,17 +278,28 @@ __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
     __shared__ uint32_t request_rows[kPlanThreads], request_tiles[kPlanThreads];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, w = tid >> 6;
     const uint32_t heads = static_cast<uint32_t>(a.cache.heads);
-    uint64_t work = 0;
+    uint64_t work = 0, ranges0 = 0;
     for (uint32_t b = tid; b < a.requests; b += kPlanThreads) {
         const Extent e = extent(a, b);
         work += static_cast<uint64_t>(row_tiles_of(a, e.tokens)) * heads * tiles_of(a, e);
     }
-    work = wave_sum(work);
-    if (lane == 0) part[w][0] = work;
+    auto block_sum = [&](uint64_t v) {
+        v = wave_sum(v);
+        __syncthreads();
+        if (lane == 0) part[w][0] = v;
+        __syncthreads();
+        v = 0;
+        for (uint32_t i = 0; i < kPlanThreads / 64; ++i) v += part[i][0];
+        return v;
+    };
+    work = block_sum(work);
+    uint32_t chunk = chunk_of(a, work, a.slots);
+    for (uint32_t b = tid; b < a.requests; b += kPlanThreads) {
+        const Extent e = extent(a, b);
+        ranges0 += static_cast<uint64_t>(row_tiles_of(a, e.tokens)) * heads * ceil_div(tiles_of(a, e), chunk);
+    }
+    if (block_sum(ranges0) > a.slots) chunk = chunk_of(a, work, 2 * a.slots);
     __syncthreads();
-    work = 0;
-    for (uint32_t i = 0; i < kPlanThreads / 64; ++i) work += part[i][0];
-    const uint32_t chunk = chunk_of(a, work);
     uint32_t items0 = 0, cuts0 = 0, joins0 = 0;  // of the requests before this batch
     for (uint32_t b0 = 0; b0 < a.requests; b0 += kPlanThreads) {
         const uint32_t b = b0 + tid;
@@ -276,11 +315,7 @@ __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
                                   ranges > 1 ? pairs : 0};
         uint64_t sum[3], all[3];
         for (int k = 0; k < 3; ++k) {
-            sum[k] = mine[k];
-            for (uint32_t d = 1; d < 64; d <<= 1) {
-                const uint64_t up = __shfl_up(sum[k], d, 64);
-                if (lane >= d) sum[k] += up;
-            }
+            sum[k] = scan_lanes(mine[k]);
         }
         __syncthreads();
         if (lane == 63)
@@ -654,18 +689,21 @@ __device__ __forceinline__ void write_row(const Args& a, const Item& item, const
 }
 
 // Zeroes the halves of four words that are not finite; whether there were any.
+// (An exponent of ones carries into the place of the sign, and no further.)
 template <class T>
 __device__ __forceinline__ bool only_finite(u32x4* x) {
-    bool found = false;
+    constexpr uint32_t kBoth = T::kExponent * 0x10001u, kOne = (T::kExponent & -T::kExponent) * 0x10001u;
+    uint32_t any = 0;
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i)
+    for (uint32_t i = 0; i < 4; ++i) any |= ((*x)[i] & kBoth) + kOne;
+    if (!(any & 0x80008000u)) return false;
 #pragma unroll
-        for (uint32_t half = 0; half < 32; half += 16)
-            if ((((*x)[i] >> half) & T::kExponent) == T::kExponent) {
-                found = true;
-                (*x)[i] &= 0xffff0000u >> half;
-            }
-    return found;
+    for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t odd = (((*x)[i] & kBoth) + kOne) & 0x80008000u;
+        if (odd & 0x8000u) (*x)[i] &= 0xffff0000u;
+        if (odd & 0x80000000u) (*x)[i] &= 0x0000ffffu;
+    }
+    return true;
 }
 
 template <class T, bool kE4M3, uint32_t kDim, uint32_t kRowWaves>
@@ -1419,7 +1457,8 @@ struct Plan {
     uint32_t dim;        // padded
     uint32_t row_waves;
     uint32_t tile_keys;
-    uint32_t target;
+    uint32_t slots;
+    uint32_t most_parts;
     uint32_t part_rows;
     uint64_t max_items, pairs;
     size_t items_offset, joins_offset, sum_offset, out_offset, bytes;
@@ -1433,17 +1472,19 @@ Plan plan_of(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t head
     const uint64_t mean = requests ? (rows + requests - 1) / requests : 0;
     p.row_waves = mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
     p.tile_keys = p.row_waves == 4 && p.dim != 256 ? 64 : 32;
-    p.target = 1024;
+    // workgroups that 256 compute units hold at once (by registers and LDS)
+    p.slots = p.dim == 256 ? 256 : 512;
     const uint64_t tile_rows = kRows * p.row_waves;
     p.part_rows = static_cast<uint32_t>(rows < tile_rows ? rows : tile_rows);
     p.pairs = heads * ((rows + tile_rows - 1) / tile_rows + requests);
-    p.max_items = 2ull * p.target + p.pairs;
+    p.most_parts = 4 * p.slots + 8;  // (a few more than the plan's lengths allow, which are rounded)
+    p.max_items = p.most_parts + p.pairs;
     auto next = [](size_t x) { return (x + 255) & ~static_cast<size_t>(255); };
     p.items_offset = 256;
     p.joins_offset = next(p.items_offset + p.max_items * sizeof(Item));
-    p.sum_offset = next(p.joins_offset + p.target * sizeof(Join));
-    p.out_offset = next(p.sum_offset + 2ull * p.target * p.part_rows * sizeof(float2));
-    p.bytes = p.out_offset + 2ull * p.target * p.part_rows * p.dim * sizeof(float);
+    p.sum_offset = next(p.joins_offset + p.most_parts / 2 * sizeof(Join));
+    p.out_offset = next(p.sum_offset + 1ull * p.most_parts * p.part_rows * sizeof(float2));
+    p.bytes = p.out_offset + 1ull * p.most_parts * p.part_rows * p.dim * sizeof(float);
     return p;
 }
 
@@ -1530,15 +1571,16 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     a.scale = scale;
     a.tile_keys = p.tile_keys;
     a.row_tile_rows = kRows * p.row_waves;
-    a.least = 512 / p.tile_keys;
+    a.slots = p.slots;
+    a.least = (p.row_waves == 1 ? 512 : 1024) / p.tile_keys;
     a.chunk_multiple = 4 / p.row_waves;
     a.part_rows = p.part_rows;
-    // the tiles that there can be at most
+    // the tiles that a pair can have at most, and the ranges that this allows
     const uint64_t tiles = (max_pages * cache->page_size + p.tile_keys - 1) / p.tile_keys +
                            (num_tokens + p.tile_keys - 1) / p.tile_keys;
     const unsigned __int128 most = static_cast<unsigned __int128>(p.pairs) * tiles / a.least + 1;
-    a.target = most < p.target ? static_cast<uint32_t>(most) : p.target;
-    a.max_items = static_cast<uint32_t>(2ull * a.target + p.pairs);
+    const uint64_t cuts = 2 * most < p.most_parts ? static_cast<uint64_t>(2 * most) : p.most_parts;
+    a.max_items = static_cast<uint32_t>(cuts + p.pairs);
     char* const ws = static_cast<char*>(workspace);
     a.head = reinterpret_cast<Head*>(ws);
     a.items = reinterpret_cast<Item*>(ws + p.items_offset);
@@ -1546,7 +1588,7 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     a.part_sum = reinterpret_cast<float2*>(ws + p.sum_offset);
     a.part_out = reinterpret_cast<float*>(ws + p.out_offset);
     // rows can be cut only if one can have more tiles than the shortest range
-    const uint64_t join_rows = static_cast<uint64_t>(a.target) * a.part_rows;
+    const uint64_t join_rows = cuts / 2 * a.part_rows;
     const uint32_t joins = tiles > a.least ? static_cast<uint32_t>(join_rows < 2048 ? join_rows : 2048) : 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (num_requests > 64) {
