@@ -161,22 +161,45 @@ __global__ __launch_bounds__(kScanThreads) void pages_count_kernel(
     if (tid == 0) *status = any_wide ? 2u : 0u;
 }
 
-// The first i in [0, n) with v[i] > t (v never decreases), n if there is none:
-// a wavefront tries 64 places at a time.
-__device__ __forceinline__ uint32_t first_past(const uint64_t* __restrict__ v, uint32_t n, uint64_t t,
-                                               uint32_t lane) {
-    uint32_t lo = 0, hi = n;  // v[i] > t for i >= hi, not for i < lo
-    while (hi - lo > 64) {
-        const uint32_t step = (hi - lo + 63) >> 6;
-        const uint64_t i = lo + static_cast<uint64_t>(lane) * step;
-        const uint64_t m = __ballot(i >= hi || v[i] > t);
-        const uint32_t f = m ? static_cast<uint32_t>(__builtin_ctzll(m)) : 64u;
-        const uint32_t end = f < 64 ? static_cast<uint32_t>(min(lo + static_cast<uint64_t>(f) * step, static_cast<uint64_t>(hi))) : hi;
-        lo = f ? lo + (f - 1) * step + 1 : lo;
-        hi = end;
+// For each of kCount values t, the first i in [0, n) with v[i] > t (v never
+// decreases), n if there is none: a wavefront tries 64 places at a time, for
+// all the values at once, so that their loads do not wait for one another.
+template <uint32_t kCount>
+__device__ __forceinline__ void first_past(const uint64_t* __restrict__ v, uint32_t n, const uint64_t* t,
+                                           uint32_t lane, uint32_t* found) {
+    uint32_t lo[kCount], hi[kCount];  // v[i] > t for i >= hi, not for i < lo
+#pragma unroll
+    for (uint32_t k = 0; k < kCount; ++k) {
+        lo[k] = 0;
+        hi[k] = n;
     }
-    const uint64_t m = __ballot(lo + lane >= hi || v[lo + lane] > t);
-    return m ? min(lo + static_cast<uint32_t>(__builtin_ctzll(m)), hi) : hi;
+    // (all intervals shrink alike: 64-fold, to a step of the one before)
+    for (uint64_t size = n; size > 64;) {
+        const uint32_t step = static_cast<uint32_t>((size + 63) >> 6);
+        uint64_t m[kCount];
+#pragma unroll
+        for (uint32_t k = 0; k < kCount; ++k) {
+            const uint64_t i = lo[k] + static_cast<uint64_t>(lane) * step;
+            m[k] = __ballot(i >= hi[k] || v[i] > t[k]);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kCount; ++k) {
+            const uint32_t f = m[k] ? static_cast<uint32_t>(__builtin_ctzll(m[k])) : 64u;
+            const uint64_t end = lo[k] + static_cast<uint64_t>(f) * step;
+            lo[k] = f ? lo[k] + (f - 1) * step + 1 : lo[k];
+            hi[k] = end < hi[k] ? static_cast<uint32_t>(end) : hi[k];
+        }
+        size = step;
+    }
+    uint64_t m[kCount];
+#pragma unroll
+    for (uint32_t k = 0; k < kCount; ++k) {
+        const uint64_t i = static_cast<uint64_t>(lo[k]) + lane;
+        m[k] = __ballot(i >= hi[k] || v[i] > t[k]);
+    }
+#pragma unroll
+    for (uint32_t k = 0; k < kCount; ++k)
+        found[k] = m[k] ? min(lo[k] + static_cast<uint32_t>(__builtin_ctzll(m[k])), hi[k]) : hi[k];
 }
 
 // The same for one lane, known to lie in [lo, hi].
@@ -227,8 +250,14 @@ __global__ __launch_bounds__(kScanThreads) void pages_take_kernel(
         all += part[0][i];
         before += part[1][i];
     }
-    // rows before the first whose sum passes the free pages are granted
-    const uint32_t granted = first_past(upto, rows, all, lane);
+    // rows before the first whose sum passes the free pages are granted; the
+    // wavefront's ranks lie between two rows
+    uint64_t r0 = before;
+    for (uint32_t i = 0; i < w; ++i) r0 += wave_free[i];
+    const uint64_t r1 = r0 + wave_free[w], wanted[3] = {all, r0, r1 ? r1 - 1 : 0};
+    uint32_t found[3];
+    first_past<3>(upto, rows, wanted, lane, found);
+    const uint32_t granted = found[0];
     const uint64_t handed = granted ? upto[granted - 1] : 0;
     if (blockIdx.x == tiles) {  // one workgroup more: the rows' own results
         bool refused = false;
@@ -241,19 +270,14 @@ __global__ __launch_bounds__(kScanThreads) void pages_take_kernel(
         if (tid == 0) *free_pages = all - handed;
         return;
     }
-    // the wavefront's ranks, and the rows that they lie between
-    uint64_t r0 = before;
-    for (uint32_t i = 0; i < w; ++i) r0 += wave_free[i];
-    const uint64_t r1 = min(r0 + wave_free[w], handed);
-    if (r0 >= r1) return;
-    const uint32_t lo = first_past(upto, granted, r0, lane);
-    const uint32_t hi = upto[lo] > r1 - 1 ? lo : first_past(upto, granted, r1 - 1, lane);
+    if (r0 >= min(r1, handed)) return;
+    const uint32_t lo = found[1], hi = min(found[2], granted - 1);
     uint64_t r = r0 + sum - own;
-    if (!own || r >= r1) return;
+    if (!own || r >= handed) return;
     uint32_t b = first_past_between(upto, lo, hi, r);
     for (uint32_t i = 0; i < kEach; ++i) {
         if (!((is_free >> i) & 1u)) continue;
-        if (r >= r1) return;
+        if (r >= handed) return;
         while (upto[b] <= r) ++b;
         const RowAsk s = ask[b];
         const uint32_t c = s.first + static_cast<uint32_t>(r - (upto[b] - s.count));
@@ -294,7 +318,7 @@ __global__ __launch_bounds__(kScanThreads) void pages_small_kernel(
     __shared__ uint32_t free_bits[kSmallPages / 32], taken_bits[kSmallPages / 32];
     __shared__ uint32_t group_rank[kSmallPages / 64];  // free pages before each 64
     __shared__ uint64_t row_upto[kSmallRows];
-    __shared__ uint32_t row_first[kSmallRows], row_need[kSmallRows], back_rows[kSmallRows];
+    __shared__ uint32_t row_first[kSmallRows], row_need[kSmallRows], row_held[kSmallRows], back_rows[kSmallRows];
     __shared__ uint64_t part[kScanThreads / 64];
     __shared__ uint32_t backs, flags, granted_rows;
     const uint32_t tid = threadIdx.x, lane = tid & 63u;
@@ -343,6 +367,7 @@ __global__ __launch_bounds__(kScanThreads) void pages_small_kernel(
         need = need_of(lengths[tid], h, &wide);
         row_first[tid] = min(h, need);
         row_need[tid] = need;
+        row_held[tid] = h;
     }
     const uint32_t count = need > h ? need - h : 0;
     __syncthreads();
@@ -371,15 +396,24 @@ __global__ __launch_bounds__(kScanThreads) void pages_small_kernel(
         for (uint32_t i = 0; i < w; ++i) before += part[i];
         if (tid < kSmallRows) row_upto[tid] = before + sum;
     }
-    // pages given back: a wavefront a row
+    // pages given back: a wavefront a row, four entries a lane at a time
     const uint32_t n_back = backs;
     for (uint32_t i = w; i < n_back; i += kScanThreads / 64) {
-        const uint32_t b = back_rows[i], first = row_need[b], last = in_use(held[b], cols);
+        const uint32_t b = back_rows[i], first = row_need[b], last = row_held[b];
         const uint64_t base = static_cast<uint64_t>(b) * cols;
-        for (uint32_t c = first + lane; c < last; c += 64) {
-            const uint32_t p = static_cast<uint32_t>(table[base + c]);
-            table_out[base + c] = -1;
-            if (p < pages) atomicOr(&free_bits[p >> 5], 1u << (p & 31u));
+        for (uint32_t c0 = first; c0 < last; c0 += 256) {
+            uint32_t p[4];
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const uint32_t c = c0 + 64 * j + lane;
+                p[j] = c < last ? static_cast<uint32_t>(table[base + c]) : ~0u;
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) {
+                const uint32_t c = c0 + 64 * j + lane;
+                if (c < last) table_out[base + c] = -1;
+                if (p[j] < pages) atomicOr(&free_bits[p[j] >> 5], 1u << (p[j] & 31u));
+            }
         }
     }
     __syncthreads();
@@ -495,13 +529,14 @@ __global__ __launch_bounds__(kThreads) void slot_map_kernel(
     for (uint64_t t0 = wave * kWaveTokens; t0 < tokens;
          t0 += static_cast<uint64_t>(gridDim.x) * (kThreads / 64) * kWaveTokens) {
         const uint64_t t1 = min(t0 + kWaveTokens, tokens) - 1;
-        const uint32_t first = first_past(offsets, rows + 1, t0, lane);
-        const uint32_t last = first <= rows && offsets[first] > t1 ? first : first_past(offsets, rows + 1, t1, lane);
+        const uint64_t ends[2] = {t0, t1};
+        uint32_t between[2];
+        first_past<2>(offsets, rows + 1, ends, lane, between);
         // a lane's consecutive tokens: the first is searched for, the others
         // mostly are of the same request
         uint64_t t = t0 + lane * kLaneTokens;
         if (t > t1) continue;
-        uint32_t at = first_past_between(offsets, first, last, t);
+        uint32_t at = first_past_between(offsets, between[0], between[1], t);
         uint64_t end = 0, length = 0;
         uint32_t used = 0;
         const int32_t* row = table;

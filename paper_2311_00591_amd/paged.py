@@ -19,7 +19,7 @@ import functools
 from typing import Optional
 
 import torch
-from torch._C import _cuda_getCurrentRawStream as _current_stream
+from torch._C import _cuda_getCurrentRawStream as _current_stream, _cuda_getDevice as _current_device
 
 from . import COOP_EVICTABLE, COOP_PINNED, _check, _ptr, load_library
 
@@ -150,7 +150,7 @@ class _Call:
             other = torch.cuda.ExternalStream(stream, self.device)
             for t in self._made:
                 t.record_stream(other)
-        if torch.cuda.current_device() == index:
+        if _current_device() == index:
             status = self._fn(*self._args, stream)
         else:
             with torch.cuda.device(self.device):
