@@ -295,6 +295,26 @@ constexpr uint32_t kSmallPages = 1u << 17;  // pages whose bits the first workgr
 constexpr uint32_t kSmallRows = kScanThreads;
 constexpr uint32_t kPageChunks = kSmallPages / 16 / kScanThreads;  // of 16 pages, a thread's
 
+// Which of 16 kinds are free, as bits: a byte is zero if adding 127 to its low
+// seven bits does not reach its top bit and that bit is zero.
+__device__ __forceinline__ uint32_t free_of(uint4 kinds) {
+    static_assert(COOP_FREE == 0, "free pages are zero bytes");
+    const uint32_t words[4] = {kinds.x, kinds.y, kinds.z, kinds.w};
+    uint32_t bits = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+        const uint32_t zero = (~(((words[i] & 0x7f7f7f7fu) + 0x7f7f7f7fu) | words[i]) >> 7) & 0x01010101u;
+        bits |= ((zero | zero >> 7 | zero >> 14 | zero >> 21) & 15u) << (4 * i);
+    }
+    return bits;
+}
+
+// The low four bits as bytes of ones.
+__device__ __forceinline__ uint32_t bytes_of(uint32_t bits) {
+    const uint32_t b = bits & 15u;
+    return ((b | b << 7 | b << 14 | b << 21) & 0x01010101u) * 0xffu;
+}
+
 // The entries of a row that neither are given back nor taken.
 __device__ __forceinline__ void copy_row(const int32_t* table, int32_t* table_out, uint64_t base,
                                          uint32_t keep, uint32_t top, uint32_t cols, uint32_t tid,
@@ -380,12 +400,7 @@ __global__ __launch_bounds__(kScanThreads) void pages_small_kernel(
             reinterpret_cast<uint16_t*>(free_bits)[c] = 0;
             continue;
         }
-        const uint32_t words[4] = {kinds[j].x, kinds[j].y, kinds[j].z, kinds[j].w};
-        uint32_t bits = 0;
-#pragma unroll
-        for (uint32_t i = 0; i < 16; ++i)
-            bits |= (((words[i >> 2] >> (8 * (i & 3))) & 0xffu) == COOP_FREE ? 1u : 0u) << i;
-        reinterpret_cast<uint16_t*>(free_bits)[c] = static_cast<uint16_t>(bits);
+        reinterpret_cast<uint16_t*>(free_bits)[c] = static_cast<uint16_t>(free_of(kinds[j]));
         reinterpret_cast<uint16_t*>(taken_bits)[c] = 0;
     }
     {   // the rows' running sum
@@ -485,11 +500,11 @@ __global__ __launch_bounds__(kScanThreads) void pages_small_kernel(
         const uint32_t is_free = reinterpret_cast<const uint16_t*>(free_bits)[c];
         const uint32_t is_taken = reinterpret_cast<const uint16_t*>(taken_bits)[c];
         uint32_t words[4] = {kinds[j].x, kinds[j].y, kinds[j].z, kinds[j].w};
+        if (is_taken | (is_free ^ free_of(kinds[j]))) {
 #pragma unroll
-        for (uint32_t i = 0; i < 16; ++i) {
-            const uint32_t at = 8 * (i & 3), mask = 0xffu << at;
-            if ((is_free >> i) & 1u)
-                words[i >> 2] = (words[i >> 2] & ~mask) | ((is_taken >> i) & 1u ? static_cast<uint32_t>(taken) << at : 0u);
+            for (uint32_t i = 0; i < 4; ++i)
+                words[i] = (words[i] & ~bytes_of(is_free >> (4 * i))) |
+                           (bytes_of(is_taken >> (4 * i)) & (taken * 0x01010101u));
         }
         if (aligned && c * 16 + 16 <= pages) {
             reinterpret_cast<uint4*>(kind_out)[c] = make_uint4(words[0], words[1], words[2], words[3]);
