@@ -1019,23 +1019,25 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
 // The attention kernel for many rows
 // ---------------------------------------------------------------------------
 
-// Four wavefronts share every tile, 32 rows each, and the matrix instructions
-// bound the work.  Tiles are brought to LDS without passing through registers,
-// in two buffers each for keys and values; a wavefront brings a quarter of
-// each tile, and one barrier a tile remains.  Operands are read from LDS a few
+// kWaves wavefronts, four or eight, share every tile, 32 rows each, and the
+// matrix instructions bound the work.  Tiles are brought to LDS without passing
+// through registers, in two buffers each for keys and values; every wavefront
+// brings its part of each tile, and one barrier a tile remains.  Eight
+// wavefronts bring each tile once for 256 rows where two workgroups of four on
+// the compute unit bring it twice, and turn to it at other times.  Operands are read from LDS a few
 // products ahead (the compiler alone reads each where it is needed, and every
 // product then waits for LDS).  8-bit tiles stay 8-bit in LDS and become
 // operands as they are read.
-template <bool kE4M3, uint32_t kDim>
+template <bool kE4M3, uint32_t kDim, uint32_t kWaves>
 struct Wide {
     static constexpr uint32_t kKeys = kDim == 256 ? 32 : 64;
     static constexpr uint32_t kChunks = kDim / 8;     // 16-byte chunks of a 16-bit row
     static constexpr uint32_t kChunks8 = kDim / 16;   // and of an 8-bit row
-    static constexpr uint32_t kOwnRows = kKeys / 4;   // rows that a wavefront brings
+    static constexpr uint32_t kOwnRows = kKeys / kWaves;   // rows that a wavefront brings
     static constexpr uint32_t kLoads = kOwnRows * kChunks / 64, kLoads8 = kOwnRows * kChunks8 / 64;
     static constexpr uint32_t kTileBytes = kKeys * kDim * 2;
     static constexpr uint32_t kSTiles = kKeys / 32, kDTiles = kDim / 32;
-    static_assert(kLoads >= 1 && kLoads8 >= 1, "every wavefront brings something");
+    static_assert(kLoads >= 1 && (!kE4M3 || kLoads8 >= 1), "every wavefront brings something");
 };
 
 // Where chunk c of an 8-bit row r lies in its row.
@@ -1069,9 +1071,9 @@ __device__ __forceinline__ void products(Read read, Multiply multiply) {
 struct Eight { static constexpr bool value = true; };   // bits of a tile's numbers
 struct Sixteen { static constexpr bool value = false; };
 
-template <class T, bool kE4M3, uint32_t kDim>
-__global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_wide_kernel(Args a) {
-    using W = Wide<kE4M3, kDim>;
+template <class T, bool kE4M3, uint32_t kDim, uint32_t kWaves>
+__global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attention_wide_kernel(Args a) {
+    using W = Wide<kE4M3, kDim, kWaves>;
     constexpr uint32_t kKeys = W::kKeys;
     constexpr uint64_t kFull = kKeys == 64 ? ~0ull : 0xffffffffull;
     __shared__ __align__(16) uint8_t keys0[W::kTileBytes], keys1[W::kTileBytes];
@@ -1213,7 +1215,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
     sight.in_lds = a.parents && e.tokens <= kParentsInLds && last > cached_tiles;
     sight.token = place.lives && last > cached_tiles ? static_cast<int32_t>(place.token) : -1;
     if (sight.in_lds)
-        for (uint32_t i = tid; i < e.tokens; i += kThreads) tree[i] = sight.parents[i];
+        for (uint32_t i = tid; i < e.tokens; i += 64 * kWaves) tree[i] = sight.parents[i];
     if (tid == 0) odd = 0;
     u32x4 q[kDim / 16];
     {
@@ -1464,16 +1466,43 @@ struct Plan {
     size_t items_offset, joins_offset, sum_offset, out_offset, bytes;
 };
 
-Plan plan_of(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t heads, uint64_t dim) {
+// The wavefronts that share every tile of keys, 32 rows each: as many as the
+// rows of an average request fill.  The lengths are on the device, the average
+// is all that the host knows of them.
+//
+// Measured with 64 requests of 200 to 4000 cached tokens, 32 query heads over 8
+// of 128 dims in bf16 (us, the fewer wavefronts first):
+//   1 or 2:   48 rows 128 : 105,    64 rows 129 : 106,    24 rows   - : 92
+//   2 or 4:   48 rows 105 : 110,    64 rows 106 : 112,    96 rows 166 : 117
+//   4 or 8:  128 rows 123 : 180,   160 rows 190 : 178,   256 rows 200 : 193,
+//            320 rows 273 : 316,   384 rows 287 : 325
+// and with 32, 16 or 8 requests
+//   4 or 8:  512 rows 197 : 183,   640 rows 242 : 251,   896 rows 318 : 309,
+//           2048 rows of one prompt 348 : 315,  4096 rows of one prompt 411 : 365.
+// So eight wavefronts pay where the rows are no more than four would be given
+// (an even number of fours), or are so many that the last tile weighs little.
+// They do not for e4m3, whose values the matrix instructions take only after
+// a conversion that every wavefront makes for itself (256 rows 190 : 196, one
+// prompt of 2048 rows 329 : 328), nor for 64 dims, where a tile is half the
+// work between two barriers (256 rows 113 : 132, one prompt of 2048 rows
+// 203 : 221); with 256 dims the sums of two wavefronts a SIMD do not fit the
+// registers.
+uint32_t row_waves_of(uint64_t mean, uint32_t dim, bool e4m3) {
+    if (mean <= 32) return 1;
+    if (mean <= 64) return 2;
+    const uint64_t fours = (mean + 4 * kRows - 1) / (4 * kRows);
+    return dim == 128 && !e4m3 && (fours % 2 == 0 || fours > 6) ? 8 : 4;
+}
+
+Plan plan_of(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t heads, uint64_t dim,
+             bool e4m3) {
     Plan p;
     p.dim = dim <= 64 ? 64 : dim <= 128 ? 128 : 256;
     const uint64_t group = q_heads / heads, rows = tokens * group;
-    // wavefronts along the rows: as many as an average request fills
-    const uint64_t mean = requests ? (rows + requests - 1) / requests : 0;
-    p.row_waves = mean <= 32 ? 1 : mean <= 64 ? 2 : 4;
-    p.tile_keys = p.row_waves == 4 && p.dim != 256 ? 64 : 32;
+    p.row_waves = row_waves_of(requests ? (rows + requests - 1) / requests : 0, p.dim, e4m3);
+    p.tile_keys = p.row_waves >= 4 && p.dim != 256 ? 64 : 32;
     // workgroups that 256 compute units hold at once (by registers and LDS)
-    p.slots = p.dim == 256 ? 256 : 512;
+    p.slots = (p.dim == 256 ? 256 : 512) / (p.row_waves == 8 ? 2 : 1);
     const uint64_t tile_rows = kRows * p.row_waves;
     p.part_rows = static_cast<uint32_t>(rows < tile_rows ? rows : tile_rows);
     p.pairs = heads * ((rows + tile_rows - 1) / tile_rows + requests);
@@ -1490,10 +1519,12 @@ Plan plan_of(uint64_t requests, uint64_t tokens, uint64_t q_heads, uint64_t head
 
 template <class T, bool kE4M3, uint32_t kDim>
 void launch(const Plan& p, const Args& a, uint32_t joins, hipStream_t s) {
+    constexpr uint32_t kMost8 = kDim == 128 && !kE4M3 ? 8 : 4;  // (others are not built)
     auto kernel = p.row_waves == 1   ? tree_attention_kernel<T, kE4M3, kDim, 1>
                   : p.row_waves == 2 ? tree_attention_kernel<T, kE4M3, kDim, 2>
-                                     : tree_attention_wide_kernel<T, kE4M3, kDim>;
-    hipLaunchKernelGGL(kernel, dim3(a.max_items), dim3(kThreads), 0, s, a);
+                  : p.row_waves == 4 ? tree_attention_wide_kernel<T, kE4M3, kDim, 4>
+                                     : tree_attention_wide_kernel<T, kE4M3, kDim, kMost8>;
+    hipLaunchKernelGGL(kernel, dim3(a.max_items), dim3(p.row_waves == 8 ? 512 : kThreads), 0, s, a);
     if (joins) {
         // the rows of all pairs: fewer than the device has wavefronts, or more
         auto join = p.pairs * p.part_rows <= 1024 ? attention_join_kernel<T, kDim, 4>
@@ -1518,8 +1549,14 @@ coop_status_t coop_tree_attention_workspace_size(uint64_t num_requests, uint64_t
                                                  size_t* bytes_out) {
     if (!bytes_out || !counts_valid(num_requests, num_tokens, q_heads, heads, dim))
         return COOP_ERR_INVALID;
-    *bytes_out =
-        num_requests && num_tokens ? plan_of(num_requests, num_tokens, q_heads, heads, dim).bytes : 0;
+    // (the pool's type, which the plan depends on, is not asked for here)
+    size_t bytes = 0;
+    if (num_requests && num_tokens)
+        for (const bool e4m3 : {false, true}) {
+            const Plan p = plan_of(num_requests, num_tokens, q_heads, heads, dim, e4m3);
+            bytes = p.bytes > bytes ? p.bytes : bytes;
+        }
+    *bytes_out = bytes;
     return COOP_OK;
 }
 
@@ -1543,7 +1580,8 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     if (!out || !coop_pages::aligned16(out) || !token_offsets) return COOP_ERR_INVALID;
     if (num_requests == 0) return COOP_OK;
     if (!lengths || (max_pages && !table)) return COOP_ERR_INVALID;
-    const Plan p = plan_of(num_requests, num_tokens, q_heads, cache->heads, cache->dim);
+    const Plan p = plan_of(num_requests, num_tokens, q_heads, cache->heads, cache->dim,
+                           cache->type == COOP_E4M3);
     if (!workspace || workspace_bytes < p.bytes) return COOP_ERR_WORKSPACE;
     Args a;
     a.q = *q;
@@ -1573,7 +1611,7 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     a.row_tile_rows = kRows * p.row_waves;
     a.slots = p.slots;
     a.least = (p.row_waves == 1 ? 512 : 1024) / p.tile_keys;
-    a.chunk_multiple = 4 / p.row_waves;
+    a.chunk_multiple = p.row_waves < 4 ? 4 / p.row_waves : 1;
     a.part_rows = p.part_rows;
     // the tiles that a pair can have at most, and the ranges that this allows
     const uint64_t tiles = (max_pages * cache->page_size + p.tile_keys - 1) / p.tile_keys +

@@ -327,6 +327,23 @@ def test_tree_attention_head_sharing(counts, q_heads, heads):
     _check_attention(a, coop.tree_attention(**a, scale=0.3), 0.3)
 
 
+@pytest.mark.parametrize("lengths, counts, q_heads, heads, dim, page", [
+    ([90, 0, 300, 70], [150, 3, 201, 61], 4, 2, 128, 16), ([64, 1], [130, 111], 2, 1, 104, 7),
+    ([1100], [129], 2, 1, 128, 24), ([20, 40] * 35, [12 + i % 20 for i in range(70)], 8, 1, 128, 16),
+    ([0, 500], [700, 530], 1, 1, 120, 64)])
+@pytest.mark.parametrize("tree", [None, "tree", "void"])
+@pytest.mark.parametrize("dtype, cache", [(BF16, BF16), (FP16, FP16), (BF16, E4M3)])
+def test_tree_attention_many_rows(lengths, counts, q_heads, heads, dim, page, tree, dtype, cache):
+    coop = _coop()
+    dim += 8 if cache == E4M3 and dim % 16 else 0  # (rows start at multiples of 16 bytes)
+    _announce(f"attention, many rows: {lengths[:4]} + {counts[:4]}, {dtype} {cache}, {tree}")
+    a = _attention_inputs(dim, lengths, counts, q_heads, heads, dim, dtype, cache, page, tree,
+                          padding=5)
+    out = torch.full((sum(counts) + 5, q_heads, dim), 7.0, dtype=dtype, device=DEV)
+    _check_attention(a, coop.tree_attention(**a, out=out))
+    assert (out[sum(counts):] == 7).all()
+
+
 @pytest.mark.parametrize("lengths, counts, heads, page", [
     ([20000], [1], 1, 16), ([9000, 12], [2, 2], 2, 24), ([5000, 0, 1, 4000], [33, 1, 70, 5], 1, 64)])
 @pytest.mark.parametrize("dtype, cache", [(BF16, BF16), (FP16, E4M3)])
@@ -338,7 +355,8 @@ def test_tree_attention_long(lengths, counts, heads, page, dtype, cache):
 
 
 @pytest.mark.parametrize("requests, longest, width, q_heads, heads", [
-    (64, 9000, 1, 32, 8), (8, 5000, 40, 16, 4), (100, 2000, 3, 8, 8), (3, 3500, 700, 8, 2)])
+    (64, 9000, 1, 32, 8), (8, 5000, 40, 16, 4), (100, 2000, 3, 8, 8), (3, 3500, 700, 8, 2),
+    (70, 900, 100, 16, 4)])
 def test_tree_attention_fills_the_device(requests, longest, width, q_heads, heads):
     """Many workgroups at once: every run gives the same bits, and rows picked
     at random are right."""
@@ -391,15 +409,18 @@ def test_tree_attention_large_scores():
         _check_attention(a, coop.tree_attention(**a, scale=-0.5), -0.5)
 
 
-@pytest.mark.parametrize("counts", [[1, 1, 1], [6, 30, 2], [70, 3, 64]])
+@pytest.mark.parametrize("counts, dim", [
+    ([1, 1, 1], 64), ([6, 30, 2], 64), ([70, 3, 64], 64), ([70, 3, 64], 128), ([140, 130, 75], 128),
+    ([140, 130, 75], 104), ([9, 130, 75], 256)])
 @pytest.mark.parametrize("dtype, cache", [(BF16, BF16), (FP16, FP16), (BF16, E4M3)])
-def test_tree_attention_sees_nothing_that_is_masked(counts, dtype, cache):
+def test_tree_attention_sees_nothing_that_is_masked(counts, dim, dtype, cache):
     """NaN and infinities in places past the lengths, on pages that are not in
     the pool, in other requests' rows and in other branches."""
     coop = _coop()
-    _announce(f"attention, NaN in masked places, {counts}")
+    dim += 8 if cache == E4M3 and dim % 16 else 0  # (rows start at multiples of 16 bytes)
+    _announce(f"attention, NaN in masked places, {counts} x {dim}")
     lengths, page = [37, 0, 90], 16
-    a = _attention_inputs(11, lengths, counts, 4, 2, 64, dtype, cache, page, "tree", padding=2)
+    a = _attention_inputs(11, lengths, counts, 4, 2, dim, dtype, cache, page, "tree", padding=2)
     nan = float("nan")
     for name in ("k_cache", "v_cache"):
         c = a[name].float()
@@ -426,7 +447,7 @@ def test_tree_attention_sees_nothing_that_is_masked(counts, dtype, cache):
     keep = np.setdiff1d(np.arange(sum(counts)), last)
     assert got[keep].isfinite().all()
     want, tol = ref.attention(a["q"], a["k"], a["v"], a["k_cache"], a["v_cache"], a["table"],
-                              a["lengths"], a["token_offsets"], a["parents"], 64 ** -0.5,
+                              a["lengths"], a["token_offsets"], a["parents"], dim ** -0.5,
                               a["k_scale"], a["v_scale"])
     assert (np.abs(got.double().cpu().numpy()[keep] - want[keep]) <= tol[keep]).all()
 
