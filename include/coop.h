@@ -12,6 +12,10 @@
  * lower start, which makes the answer unique.  S == 0 gives the empty window
  * {0, 0, 0}; a request no window satisfies gives {~0, ~0, ~0}.
  *
+ * The last section has the operators on paged pools: block tables and slot
+ * maps over a pool's pages, the keys and values kept there, and the attention
+ * that reads them.
+ *
  * The library is stateless apart from a per-process call counter, allocates
  * nothing, never synchronises the stream, and may be called from several
  * host threads (with distinct workspaces).  It needs no HIP header: streams
@@ -372,7 +376,8 @@ coop_status_t coop_replay(uint64_t *size, uint64_t *cost, uint8_t *kind, uint32_
  *   1 if one needed more than max_pages.  free_pages (device u64): the free
  *   pages left.
  * workspace: coop_page_tables_workspace_size() bytes (device, 256-byte
- *   aligned, caller-owned, contents need not be initialised).  num_pages,
+ *   aligned, caller-owned, contents need not be initialised); 0, and workspace
+ *   may be NULL, for at most 2^17 pages and 2^10 requests.  num_pages,
  *   num_requests and max_pages are at most 2^31 - 1 each, and page_size at
  *   least 1.  With num_requests == 0 the free pages are still counted.
  */
@@ -472,8 +477,9 @@ coop_status_t coop_cache_write(const coop_rows_t *k, const coop_rows_t *v, int32
  *
  * q, k_new, v_new, out: `type` (COOP_BF16 or COOP_FP16); the cache has the
  * same type or COOP_E4M3.  q_heads is a multiple of cache->heads.  out
- * (device, 16-byte aligned): [num_tokens][q_heads][dim], without gaps; rows
- * past token_offsets[num_requests] are left as they were.
+ * (device, 16-byte aligned): [num_tokens][q_heads][dim], without gaps; it must
+ * not overlap any input, and rows past token_offsets[num_requests] are left as
+ * they were.
  * workspace: coop_tree_attention_workspace_size() bytes (device, 256-byte
  * aligned, caller-owned, contents need not be initialised); two calls in
  * flight at the same time must not share one.

@@ -570,6 +570,104 @@ def test_another_stream():
     assert torch.equal(got, want)
 
 
+def test_two_streams_at_once():
+    """Calls of two streams that run at the same time, with a workspace each."""
+    coop = _coop()
+    _announce("two streams")
+    a = [_attention_inputs(41, [9000, 4000, 2500], [9, 9, 20], 8, 2, 128, BF16, BF16, 16, "tree"),
+         _attention_inputs(42, [3000] * 70, [2] * 70, 8, 4, 64, FP16, FP16, 16, None)]
+    want = [coop.tree_attention(**x) for x in a]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in a]
+    calls = [coop.TreeAttention(**x) for x in a]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for call, stream in zip(calls, streams):
+            call.launch(stream.cuda_stream)
+    torch.cuda.synchronize()
+    for call, x in zip(calls, want):
+        assert torch.equal(call.out, x)
+
+
+@pytest.mark.parametrize("requests, tokens", [(3, 5), (80, 1), (3, 150)])
+def test_attention_captured_and_replayed(requests, tokens):
+    """Replays take their lengths, trees and tables from the device."""
+    coop = _coop()
+    _announce(f"attention of {requests} requests captured")
+    made = [_attention_inputs(50 + i, [(i + 1) * 100 + 7 * b for b in range(requests)],
+                              [tokens] * requests, 4, 2, 128, BF16, BF16, 16, tree, cols=80)
+            for i, tree in enumerate(("tree", "chain", "void"))]
+    pages = max(x["k_cache"].shape[0] for x in made)
+    a = {n: torch.zeros_like(x) for n, x in made[0].items() if x is not None}
+    for n in ("k_cache", "v_cache"):
+        a[n] = torch.zeros((pages, *a[n].shape[1:]), dtype=BF16, device=DEV)
+    a["table"].fill_(-1)
+    a["parents"].fill_(-1)
+    coop.tree_attention(**a)  # (loads the kernels)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = coop.tree_attention(**a)
+    for x in made + made[:1]:
+        for n, to in a.items():
+            to[:x[n].shape[0]].copy_(x[n])
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, coop.tree_attention(**x))
+    _check_attention(made[0], out)
+
+
+@pytest.mark.parametrize("counts", [[1, 2, 1], [30, 9, 25], [200, 3, 180]])
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+def test_keys_and_values_laid_out_apart(counts, cache):
+    """Other strides for the keys than for the values, and pages that two
+    requests share: the same bits as from one plain layout."""
+    coop = _coop()
+    _announce(f"keys and values laid out apart, {counts}")
+    a = _attention_inputs(61, [130, 50, 130], counts, 6, 3, 128, BF16, cache, 16, "tree")
+    a["table"][2] = a["table"][0]
+    want = coop.tree_attention(**a)
+    _check_attention(a, want)
+    raw = a["k_cache"].view(torch.uint8 if cache == E4M3 else torch.int16)
+    a["k_cache"] = raw.transpose(1, 2).contiguous().transpose(1, 2).view(cache)
+    assert a["k_cache"].stride() != a["v_cache"].stride()
+    assert torch.equal(coop.tree_attention(**a), want)
+
+
+@pytest.mark.parametrize("cache", [BF16, E4M3])
+def test_pools_past_32_bits(cache):
+    """Pools of more than 2^32 elements for each of keys and values."""
+    coop = _coop()
+    pages, page, heads, dim = 300_000, 16, 8, 128
+    assert pages * page * heads * dim > 2**32
+    _announce(f"a pool past 32 bits, {cache}")
+    raw = torch.uint8 if cache == E4M3 else BF16
+    far = (torch.empty((pages, page, heads, dim), dtype=raw, device=DEV).view(cache),
+           torch.empty((heads, pages, page, dim), dtype=raw, device=DEV).permute(1, 2, 0, 3).view(cache))
+    near = tuple(torch.empty((16, page, heads, dim), dtype=raw, device=DEV).view(cache) for _ in "kv")
+    where = [299_999, 5, 150_000, 262_143, 262_144, 262_145, 131_071, 131_072, 280_000, 0, 299_998, 77]
+    scales = {}
+    if cache == E4M3:
+        scales = {n: torch.full((heads,), 0.01, device=DEV) for n in ("k_scale", "v_scale")}
+    g = torch.Generator(device=DEV).manual_seed(1)
+    k, v = (torch.randn((192, heads, dim), generator=g, device=DEV, dtype=BF16) for _ in "kv")
+    place = torch.arange(192, device=DEV)
+    coop.cache_write(k, v, place, *near, **scales)
+    coop.cache_write(k, v, _ints(where)[place // page] * page + place % page, *far, **scales)
+    for x, y in zip(far, near):
+        got = torch.stack([x[p].contiguous().view(torch.uint8) for p in where])
+        assert torch.equal(got, y[:12].view(torch.uint8).view_as(got))
+    lengths = _ints([100, 80])
+    table = torch.full((2, 8), -1, dtype=torch.int32, device=DEV)
+    table[0, :7], table[1, :5] = _ints(range(7), torch.int32), _ints(range(7, 12), torch.int32)
+    moved = torch.where(table < 0, table, _ints(where, torch.int32)[table.clamp(min=0)])
+    for n in (1, 9, 80):
+        q = torch.randn((2 * n, 2 * heads, dim), generator=g, device=DEV, dtype=BF16)
+        k, v = (torch.randn((2 * n, heads, dim), generator=g, device=DEV, dtype=BF16) for _ in "kv")
+        offsets = _ints([0, n, 2 * n])
+        want = coop.tree_attention(q, k, v, *near, table, lengths, offsets, **scales)
+        assert torch.equal(coop.tree_attention(q, k, v, *far, moved, lengths, offsets, **scales), want)
+
+
 class _Server:
     """Sequences in a pool, a decoding step with drafted trees at a time, on
     the package and on the reference."""
