@@ -88,7 +88,7 @@ struct Args {
     uint32_t page_bytes, place_bytes;
     float scale;
     // the plan and the workspace
-    uint32_t tile_keys, row_tile_rows, slots, least, chunk_multiple, max_items, part_rows;
+    uint32_t tile_keys, row_tile_rows, slots, least, least_more, chunk_multiple, max_items, part_rows;
     Head* head;
     Item* items;
     Join* joins;
@@ -158,16 +158,32 @@ __device__ __forceinline__ U wave_sum(U v) { return from_lane(scan_lanes(v), 63)
 
 // Pairs (a request's row tile and head) of many tiles are cut into ranges of
 // `chunk` tiles, all of one length.  Workgroups take ranges as they come free,
-// a.slots of them at once.  If ranges that cut the whole work evenly among the
-// slots all fit at once, they end together; where pairs leave too many
-// remainders for that, ranges of half the length keep the wait for the last
-// ones short.  Shorter ones yet cost more in starts, ends and joins than they
-// save (and this plan, which every wavefront makes, has to be short itself).
-// Ranges no shorter than W / n tiles, W the whole work, leave at most 2 n parts.
-__device__ __forceinline__ uint32_t chunk_of(const Args& a, uint64_t work, uint32_t slots) {
+// a.slots of them at once.
+//  - If ranges that cut the whole work W evenly among the slots all fit at
+//    once, they end together; 128 keys at least, where all fit anyhow: a start,
+//    an end and a part to join cost as much as some 200 keys.  With 512 keys at
+//    least, four sequences of 100 to 700 tokens took 14.2 us for 11.0, one tree
+//    of 64 tokens after 1000 (32 heads over 8 of 128 dims) 31 us for 23, after
+//    8000 34 us for 33.
+//  - Where pairs leave too many remainders for that, ranges of half the length
+//    keep the wait for the last ones short, 1024 keys at least: 48 trees over
+//    e4m3 keys took 119 us for 109 with 512 and 124 us with 2048, 64 trees of
+//    12 tokens 132 and 148 for 126, 64 single tokens the same 234 with each.
+//    Even ranges throughout took 260 us for the last.
+// Other lengths, tried until their ranges fit, gained less than this plan grew,
+// which every wavefront makes: 64 single tokens took 241 us for 234.
+// Ranges no shorter than W / n tiles leave at most 2 n parts.
+__device__ __forceinline__ uint32_t chunk_of(const Args& a, uint64_t work, uint32_t slots, uint32_t least) {
     const float even = ceilf(static_cast<float>(work) / static_cast<float>(slots)) + 1.f;
-    const uint32_t n = even < 0x1p30f ? max(static_cast<uint32_t>(even), a.least) : 1u << 30;
+    const uint32_t n = even < 0x1p30f ? max(static_cast<uint32_t>(even), least) : 1u << 30;
     return (n + a.chunk_multiple - 1) / a.chunk_multiple * a.chunk_multiple;
+}
+
+// (`ranges(n)`: how many ranges of n tiles there are)
+template <class Ranges>
+__device__ __forceinline__ uint32_t chunk_of(const Args& a, uint64_t work, Ranges ranges) {
+    const uint32_t even = chunk_of(a, work, a.slots, a.least);
+    return ranges(even) <= a.slots ? even : chunk_of(a, work, 2 * a.slots, a.least_more);
 }
 
 __device__ __forceinline__ uint32_t row_tiles_of(const Args& a, uint32_t tokens) {
@@ -194,8 +210,7 @@ __device__ __forceinline__ LanePlan lane_plan(const Args& a, uint32_t lane) {
     p.tiles = tiles_of(a, p.e);
     p.pairs = row_tiles_of(a, p.e.tokens) * heads;
     const uint64_t work = wave_sum(static_cast<uint64_t>(p.pairs) * p.tiles);
-    p.chunk = chunk_of(a, work, a.slots);
-    if (wave_sum(p.pairs * ceil_div(p.tiles, p.chunk)) > a.slots) p.chunk = chunk_of(a, work, 2 * a.slots);
+    p.chunk = chunk_of(a, work, [&](uint32_t n) { return wave_sum(p.pairs * ceil_div(p.tiles, n)); });
     p.ranges = ceil_div(p.tiles, p.chunk);
     const bool cut = p.ranges > 1;
     p.items = scan_lanes(p.pairs * p.ranges);
@@ -278,7 +293,7 @@ __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
     __shared__ uint32_t request_rows[kPlanThreads], request_tiles[kPlanThreads];
     const uint32_t tid = threadIdx.x, lane = tid & 63u, w = tid >> 6;
     const uint32_t heads = static_cast<uint32_t>(a.cache.heads);
-    uint64_t work = 0, ranges0 = 0;
+    uint64_t work = 0;
     for (uint32_t b = tid; b < a.requests; b += kPlanThreads) {
         const Extent e = extent(a, b);
         work += static_cast<uint64_t>(row_tiles_of(a, e.tokens)) * heads * tiles_of(a, e);
@@ -293,12 +308,14 @@ __global__ __launch_bounds__(kPlanThreads) void attention_plan_kernel(Args a) {
         return v;
     };
     work = block_sum(work);
-    uint32_t chunk = chunk_of(a, work, a.slots);
-    for (uint32_t b = tid; b < a.requests; b += kPlanThreads) {
-        const Extent e = extent(a, b);
-        ranges0 += static_cast<uint64_t>(row_tiles_of(a, e.tokens)) * heads * ceil_div(tiles_of(a, e), chunk);
-    }
-    if (block_sum(ranges0) > a.slots) chunk = chunk_of(a, work, 2 * a.slots);
+    const uint32_t chunk = chunk_of(a, work, [&](uint32_t n) {
+        uint64_t ranges = 0;
+        for (uint32_t b = tid; b < a.requests; b += kPlanThreads) {
+            const Extent e = extent(a, b);
+            ranges += static_cast<uint64_t>(row_tiles_of(a, e.tokens)) * heads * ceil_div(tiles_of(a, e), n);
+        }
+        return block_sum(ranges);
+    });
     __syncthreads();
     uint32_t items0 = 0, cuts0 = 0, joins0 = 0;  // of the requests before this batch
     for (uint32_t b0 = 0; b0 < a.requests; b0 += kPlanThreads) {
@@ -1610,7 +1627,8 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     a.tile_keys = p.tile_keys;
     a.row_tile_rows = kRows * p.row_waves;
     a.slots = p.slots;
-    a.least = (p.row_waves == 1 ? 512 : 1024) / p.tile_keys;
+    a.least = 128 / p.tile_keys;
+    a.least_more = 1024 / p.tile_keys;
     a.chunk_multiple = p.row_waves < 4 ? 4 / p.row_waves : 1;
     a.part_rows = p.part_rows;
     // the tiles that a pair can have at most, and the ranges that this allows
