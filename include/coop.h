@@ -377,7 +377,7 @@ coop_status_t coop_replay(uint64_t *size, uint64_t *cost, uint8_t *kind, uint32_
  *   pages left.
  * workspace: coop_page_tables_workspace_size() bytes (device, 256-byte
  *   aligned, caller-owned, contents need not be initialised); 0, and workspace
- *   may be NULL, for at most 2^17 pages and 2^10 requests.  num_pages,
+ *   may be NULL, for at most 2^17 pages and 2^9 requests.  num_pages,
  *   num_requests and max_pages are at most 2^31 - 1 each, and page_size at
  *   least 1.  With num_requests == 0 the free pages are still counted.
  */

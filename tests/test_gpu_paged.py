@@ -62,7 +62,7 @@ def _check_tables(got, want):
 @pytest.mark.parametrize("pages, rows, cols, page, free, tight", [
     (1, 1, 1, 1, 1.0, 1.0), (64, 1, 70, 16, 0.5, 2.0), (63, 5, 1, 16, 0.5, 0.5),
     (1000, 7, 130, 16, 0.6, 0.4), (4096, 64, 33, 7, 0.3, 1.5), (4097, 300, 20, 16, 0.9, 0.5),
-    (20000, 1500, 9, 128, 0.5, 1.1), (131072, 1024, 60, 16, 0.6, 0.9), (131073, 9, 800, 16, 0.2, 1.0),
+    (20000, 1500, 9, 128, 0.5, 1.1), (131072, 512, 60, 16, 0.6, 0.9), (131072, 513, 60, 16, 0.6, 0.9), (131073, 9, 800, 16, 0.2, 1.0),
     (5000, 1000, 40, 48, 0.95, 0.1), (70000, 40, 2500, 16, 0.7, 0.7),
     (300001, 1025, 400, 1, 0.8, 0.9)])
 def test_page_tables(pages, rows, cols, page, free, tight):
