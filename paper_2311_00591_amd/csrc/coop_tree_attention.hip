@@ -1256,6 +1256,8 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
     const float cached_scale = kE4M3 ? new_scale * a.cache.k_scale[item.head] : new_scale;
     const float value_scale = kE4M3 ? a.cache.v_scale[item.head] : 1.f;
     bool scaled = false;  // whether o has met the cached values' scale
+    // a wavefront without rows brings its part of the tiles and does nothing else
+    const bool works = __ballot(place.lives) != 0;
 
     // an operand as it is read, and as products take it
     auto operand = [](u32x4 x, auto width) -> u32x4 {
@@ -1333,6 +1335,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
         next = locate(tile + 2, page);
         page = page_of(tile + 3);
 
+        if (!works) return;
         f32x16 s[W::kSTiles];
         scores(keys, s, width);
         uint64_t sees = counts;
