@@ -15,6 +15,12 @@
 //     first row whose running sum exceeds r, if that sum is at most the number
 //     of free pages: nothing is listed or sorted, each page finds its own row.
 //
+// What bounds it.  A small pool is a chain of some ten dependent steps of one
+// workgroup: 6.5 us for 8 sequences on 600 pages, 19 us for 512 on 107 thousand
+// (4.9 MB in all).  A large one is four launches, each with its start and its
+// searches: 2.5, 7.9, 5.8 and 11.8 us for 4096 sequences on 772 thousand pages,
+// where 44 MB are moved, 9 us at the rate of a large copy.
+//
 // coop_slot_map and coop_cache_write are one launch each.
 
 #include <hip/hip_runtime.h>
@@ -532,7 +538,9 @@ __global__ __launch_bounds__(kThreads) void pages_small_rows_kernel(
 // One wavefront takes 256 consecutive tokens at a time.  The requests of its
 // first and last token are found together, 64 probes at a time, and its lanes
 // search between the two: tokens of a prompt share their request, and single
-// tokens of 64 requests are six steps apart.
+// tokens of 64 requests are six steps apart.  Loads that depend on one another
+// bound it: 4.3 us for 8 tokens, 10.8 us for 1.2 million of 4096
+// sequences.
 __global__ __launch_bounds__(kThreads) void slot_map_kernel(
     const int32_t* __restrict__ table, uint32_t rows, uint32_t cols,
     const int32_t* __restrict__ held, const uint64_t* __restrict__ lengths,
@@ -638,7 +646,9 @@ struct WriteArgs {
 };
 
 // A thread takes a chunk (eight elements) of a token's key row and the same of
-// its value row; consecutive threads take consecutive chunks.
+// its value row; consecutive threads take consecutive chunks.  Memory bounds it:
+// 65536 tokens of 8 heads of 128 into an e4m3 pool, 383 MB, take 84.6 us (4.5
+// TB/s), 64 tokens 2.7 us.  Divisions of 64 bits and by the scales took 109 us.
 template <bool kE4M3>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(WriteArgs a) {
     const coop_cache_t& cache = a.cache;
