@@ -1070,7 +1070,10 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
 // that no row sees left out of the count.  Without the products the softmax
 // alone would take some 60 % of that, and the two do not overlap within a
 // wavefront: taking the scores of the next tile ahead needs more registers than
-// there are (760 us, spilled).  48 trees of 1 to 40 tokens over e4m3 take 108
+// there are (760 us, spilled); two sets of wavefronts that take turns, one at
+// the products while the other weighs, came to 415 us.  The lambdas are inlined
+// by force, which decides what stays in registers (64 trees of 32 tokens, heads
+// of 256: 291 us for 310).  48 trees of 1 to 40 tokens over e4m3 take 108
 // us: 1.6 TB/s, 340 TFLOP/s.
 template <bool kE4M3, uint32_t kDim, uint32_t kWaves>
 struct Wide {
@@ -1114,6 +1117,8 @@ __device__ __forceinline__ void products(Read read, Multiply multiply) {
 
 struct Eight { static constexpr bool value = true; };   // bits of a tile's numbers
 struct Sixteen { static constexpr bool value = false; };
+struct Keys { static constexpr bool value = true; };     // what is brought
+struct Values { static constexpr bool value = false; };
 
 template <class T, bool kE4M3, uint32_t kDim, uint32_t kWaves>
 __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attention_wide_kernel(Args a) {
@@ -1151,7 +1156,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
     const uint32_t my_key = lane % kKeys;
     const uint32_t table_end = min(cached_tiles, last) * kKeys < e.cached ? min(cached_tiles, last) * kKeys : e.cached;
     const int32_t* const table = a.table + static_cast<uint64_t>(item.request) * a.max_pages;
-    auto page_of = [&](uint32_t tile) -> int32_t {
+    auto page_of = [&](uint32_t tile) __attribute__((always_inline)) -> int32_t {
         const uint32_t pos = tile * kKeys + my_key;
         return pos < table_end ? table[page_at(pos)] : -1;
     };
@@ -1159,7 +1164,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
         uint64_t k, v;
         uint64_t counts;  // which of the tile's keys count
     };
-    auto locate = [&](uint32_t tile, int32_t page) {
+    auto locate = [&](uint32_t tile, int32_t page) __attribute__((always_inline)) {
         Where r = {kNowhere, kNowhere, 0};
         if (tile < cached_tiles) {
             const uint32_t pos = tile * kKeys + my_key;
@@ -1184,7 +1189,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
         r.counts = kKeys == 64 ? all : all & 0xffffffffu;
         return r;
     };
-    auto from = [&](uint64_t v, uint32_t r) -> uint64_t {
+    auto from = [&](uint64_t v, uint32_t r) __attribute__((always_inline)) -> uint64_t {
         return static_cast<uint64_t>(__shfl(static_cast<uint32_t>(v), r, 64)) |
                static_cast<uint64_t>(__shfl(static_cast<uint32_t>(v >> 32), r, 64)) << 32;
     };
@@ -1192,46 +1197,46 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
         __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
                                          (__attribute__((address_space(3))) void*)to, 16, 0, 0);
     };
-    // Brings this wavefront's rows of a tile: lane by lane to consecutive
-    // chunks of LDS, so each lane fetches the chunk whose place that is.
-    auto bring = [&](uint32_t tile, const Where& at, uint8_t* keys, uint8_t* values) {
+    // Brings this wavefront's rows of a tile's keys or values: lane by lane to
+    // consecutive chunks of LDS, so each lane fetches the chunk whose place that
+    // is.
+    auto bring = [&](uint32_t tile, uint64_t offset, uint64_t counts, Global cache_base, Global new_base,
+                     uint8_t* to, auto of_keys) __attribute__((always_inline)) {
         if (tile >= last) return;
-        const bool cached = tile < cached_tiles, same = cached && a.narrow;
-        const bool plain = dim == kDim && at.counts == kFull;  // nothing is zeroed
-        auto rows_of = [&](uint32_t r, Global kb, Global vb, Global* k, Global* v) {
-            const uint64_t ok = from(at.k, r), ov = same ? ok : from(at.v, r);
-            *k = kb + ok;
-            *v = vb + ov;
-            if (!plain && ok == kNowhere) *k = *v = zeros;
+        const bool cached = tile < cached_tiles;
+        const bool plain = dim == kDim && counts == kFull;  // nothing is zeroed
+        const Global base = cached ? cache_base : new_base;
+        auto row_of = [&](uint32_t r) {
+            const uint64_t at = from(offset, r);
+            return !plain && at == kNowhere ? zeros : base + at;
         };
         if (kE4M3 && cached) {
 #pragma unroll
             for (uint32_t j = 0; j < W::kLoads8; ++j) {
                 const uint32_t slot = j * 64 + lane, r = w * W::kOwnRows + slot / W::kChunks8;
                 const uint32_t c = chunk_of_8<kDim>(r, slot % W::kChunks8) * 16;
-                const uint32_t to = (w * W::kOwnRows * W::kChunks8 + j * 64) * 16;
-                Global k, v;
-                rows_of(r, ck, cv, &k, &v);
-                fetch(plain || c < dim ? k + c : zeros, keys + to);
-                fetch(plain || c < dim ? v + c : zeros, values + to);
+                const Global row = row_of(r);
+                fetch(plain || c < dim ? row + c : zeros, to + (w * W::kOwnRows * W::kChunks8 + j * 64) * 16);
             }
         } else {
-            const Global kb = cached ? ck : nk, vb = cached ? cv : nv;
 #pragma unroll
             for (uint32_t j = 0; j < W::kLoads; ++j) {
                 const uint32_t slot = j * 64 + lane, r = w * W::kOwnRows + slot / W::kChunks;
-                const uint32_t ks = key_chunk<kDim>(r, slot % W::kChunks) * 16;
-                const uint32_t vs = value_chunk<kDim>(r, slot % W::kChunks) * 16;
-                const uint32_t to = (w * W::kOwnRows * W::kChunks + j * 64) * 16;
-                Global k, v;
-                rows_of(r, kb, vb, &k, &v);
-                fetch(plain || ks < 2 * dim ? k + ks : zeros, keys + to);
-                fetch(plain || vs < 2 * dim ? v + vs : zeros, values + to);
+                const uint32_t c = (decltype(of_keys)::value ? key_chunk<kDim>(r, slot % W::kChunks)
+                                                             : value_chunk<kDim>(r, slot % W::kChunks)) * 16;
+                const Global row = row_of(r);
+                fetch(plain || c < 2 * dim ? row + c : zeros, to + (w * W::kOwnRows * W::kChunks + j * 64) * 16);
             }
         }
     };
+    auto bring_keys = [&](uint32_t tile, const Where& at, uint8_t* to) __attribute__((always_inline)) {
+        bring(tile, at.k, at.counts, ck, nk, to, Keys());
+    };
+    auto bring_values = [&](uint32_t tile, const Where& at, uint8_t* to) __attribute__((always_inline)) {
+        bring(tile, at.v, at.counts, cv, nv, to, Values());
+    };
     // Takes out of this wavefront's rows of new values what is not finite.
-    auto clean = [&](uint8_t* values) {
+    auto clean = [&](uint8_t* values) __attribute__((always_inline)) {
 #pragma unroll
         for (uint32_t j = 0; j < W::kLoads; ++j) {
             u32x4* const p = reinterpret_cast<u32x4*>(values) + w * W::kOwnRows * W::kChunks + j * 64 + lane;
@@ -1251,7 +1256,8 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
     const int32_t first_page = page_of(first), second_page = page_of(first + 1);
     int32_t page = page_of(first + 2);
     Where now = locate(first, first_page);  // of the tile that is next
-    bring(first, now, keys0, values0);
+    bring_keys(first, now, keys0);
+    bring_values(first, now, values0);
 
     Sight sight;
     sight.parents = a.parents ? a.parents + e.first : nullptr;
@@ -1295,7 +1301,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
             return x;
     };
     // the products of a tile's keys with the rows' queries
-    auto scores = [&](const uint8_t* __restrict__ keys, f32x16* to, auto width) {
+    auto scores = [&](const uint8_t* __restrict__ keys, f32x16* to, auto width) __attribute__((always_inline)) {
 #pragma unroll
         for (uint32_t t = 0; t < W::kSTiles; ++t)
 #pragma unroll
@@ -1318,7 +1324,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
             });
     };
     // adds a tile's values by their weights
-    auto add = [&](const uint8_t* __restrict__ values, uint32_t (*p)[8], auto width) {
+    auto add = [&](const uint8_t* __restrict__ values, uint32_t (*p)[8], auto width) __attribute__((always_inline)) {
         const uint32_t g = lane & 15u;
         products<2 * W::kSTiles * W::kDTiles>(
             [&](uint32_t i) -> u32x4 {
@@ -1348,23 +1354,10 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
                 o[dt] = T::mfma(operand(x, width), px, o[dt]);
             });
     };
-    // A tile, on its way to `keys` and `values`.
-    auto step = [&](uint32_t tile, auto width, uint8_t* __restrict__ keys, uint8_t* __restrict__ values,
-                    uint8_t* __restrict__ keys_to, uint8_t* __restrict__ values_to) {
+    // The weights of a tile's scores; moves the sums' base.
+    auto weigh = [&](uint32_t tile, uint64_t counts, f32x16* s, uint32_t (*p)[8], auto width) __attribute__((always_inline)) {
         constexpr bool kNew = kE4M3 && !decltype(width)::value;  // (a 16-bit tile of an 8-bit cache's call)
         const bool is_new = kNew || tile >= cached_tiles;
-        arrived();
-        if (is_new) clean(values);
-        __syncthreads();
-        const uint64_t counts = now.counts;
-        bring(tile + 1, next, keys_to, values_to);
-        now = next;
-        next = locate(tile + 2, page);
-        page = page_of(tile + 3);
-
-        if (!works) return;
-        f32x16 s[W::kSTiles];
-        scores(keys, s, width);
         uint64_t sees = counts;
         if (is_new) sees = sight.of_tile<kKeys>(static_cast<int32_t>((all_tiles - 1 - tile) * kKeys));
         float factor = is_new ? new_scale : cached_scale;
@@ -1378,8 +1371,32 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
             for (uint32_t t = 0; t < W::kDTiles; ++t)
 #pragma unroll
                 for (uint32_t i = 0; i < 16; ++i) o[t][i] *= grow;
-        uint32_t p[W::kSTiles][8];
         l += weights_of<T, W::kSTiles>(s, factor, m, p);
+    };
+    // The page's number is there as all that was brought is.  Said ahead of what
+    // is brought next: a wait for it later would be one for that too.
+    auto located = [&](uint32_t tile) __attribute__((always_inline)) {
+        asm volatile("" : "+v"(page));
+        return locate(tile, page);
+    };
+    // A tile, on its way to `keys` and `values`.
+    auto step = [&](uint32_t tile, auto width, uint8_t* __restrict__ keys, uint8_t* __restrict__ values,
+                    uint8_t* __restrict__ keys_to, uint8_t* __restrict__ values_to) __attribute__((always_inline)) {
+        arrived();
+        if ((kE4M3 && !decltype(width)::value) || tile >= cached_tiles) clean(values);
+        __syncthreads();
+        const uint64_t counts = now.counts;
+        const Where after = located(tile + 2);
+        bring_keys(tile + 1, next, keys_to);
+        bring_values(tile + 1, next, values_to);
+        now = next;
+        next = after;
+        page = page_of(tile + 3);
+        if (!works) return;
+        f32x16 s[W::kSTiles];
+        uint32_t p[W::kSTiles][8];
+        scores(keys, s, width);
+        weigh(tile, counts, s, p, width);
         add(values, p, width);
     };
     __syncthreads();  // (the tree, and that no value is odd yet)
