@@ -448,7 +448,8 @@ typedef struct {
  * cache's unless that is COOP_E4M3: then an element is divided by its head's
  * scale in 32 bits, limited to +-448 and rounded to nearest, ties to even
  * (NaN stays NaN).  A token whose slot is negative or past the pool is
- * skipped.  Slots given twice leave one of the rows, or parts of several.
+ * skipped.  Slots given twice leave one of the rows, or parts of several.  k and
+ * v must not overlap the places that are written.
  */
 coop_status_t coop_cache_write(const coop_rows_t *k, const coop_rows_t *v, int32_t type,
                                const int64_t *slots, uint64_t num_tokens,

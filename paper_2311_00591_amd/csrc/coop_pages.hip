@@ -775,6 +775,7 @@ coop_status_t coop_page_tables(const uint8_t* kind, uint64_t num_pages, const in
     }
     const TablesLayout l = tables_layout(num_pages, num_requests);
     if (l.bytes && (!workspace || workspace_bytes < l.bytes)) return COOP_ERR_WORKSPACE;
+    if (l.bytes && !coop_pages::aligned16(workspace)) return COOP_ERR_INVALID;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const uint32_t pages = static_cast<uint32_t>(num_pages), rows = static_cast<uint32_t>(num_requests);
     const uint32_t cols = static_cast<uint32_t>(max_pages);

@@ -1650,6 +1650,7 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
     const Plan p = plan_of(num_requests, num_tokens, q_heads, cache->heads, cache->dim,
                            cache->type == COOP_E4M3);
     if (!workspace || workspace_bytes < p.bytes) return COOP_ERR_WORKSPACE;
+    if (!coop_pages::aligned16(workspace)) return COOP_ERR_INVALID;
     Args a;
     a.q = *q;
     a.k = *k_new;

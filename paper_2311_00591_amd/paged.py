@@ -11,6 +11,8 @@ and as a function.
 Caches are tensors [pages, page_size, heads, dim] of bfloat16, float16 or
 float8_e4m3fn, in any order of the first three dimensions in memory (a
 transposed view, or one half of a tensor that holds keys and values together).
+
+The operators serve a model that answers; no gradients are recorded.
 """
 from __future__ import annotations
 

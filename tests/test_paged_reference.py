@@ -68,9 +68,10 @@ def test_page_tables_refusals():
     for name in ("kind", "table", "held", "lengths", "table_out", "held_out", "kind_out", "status",
                  "free"):
         assert call(**{name: None}) == -1, name
-    # (a pool of up to 2^17 pages and 2^10 rows needs no workspace)
-    for large in (dict(pages=1 << 20), dict(rows=1025)):
+    # (a pool of up to 2^17 pages and 2^9 rows needs no workspace)
+    for large in (dict(pages=1 << 20), dict(rows=513)):
         assert call(ws=None, **large) == -2 and call(wsb=8, **large) == -2
+        assert call(ws=0xa000008, **large) == -1
     assert call(page=0) == -1 and call(taken=0) == -1 and call(taken=3) == -1
     for big in ("pages", "rows", "cols"):
         assert call(**{big: 1 << 31}) == -1, big
@@ -148,7 +149,8 @@ def test_tree_attention_refusals():
     assert call(type=2) == -1
     for name in ("off", "table", "lengths", "out"):
         assert call(**{name: None}) == -1, name
-    assert call(out=NZ + 8) == -1
+    assert call(out=NZ + 8) == -1 and call(ws=NZ + 8) == -1
+    assert call(ws=None) == -2 and call(wsb=4096) == -2
     assert call(q_heads=5) == -1 and call(q_heads=0) == -1
     assert call(tokens=1 << 30) == -1 and call(requests=1 << 31) == -1 and call(cols=1 << 31) == -1
     assert _lib().coop_tree_attention(None, None, None, 0, 4, 3, NZ, None, None, NZ, 4, NZ, 2, 1.0,
