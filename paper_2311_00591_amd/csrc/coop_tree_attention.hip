@@ -1071,7 +1071,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
 // alone would take some 60 % of that, and the two do not overlap within a
 // wavefront: taking the scores of the next tile ahead needs more registers than
 // there are (760 us, spilled); two sets of wavefronts that take turns, one at
-// the products while the other weighs, came to 415 us.  The lambdas are inlined
+// the products while the other weighs, came to 391 us and cost the other calls
+// here 3 to 10 %.  The lambdas are inlined
 // by force, which decides what stays in registers (64 trees of 32 tokens, heads
 // of 256: 291 us for 310).  48 trees of 1 to 40 tokens over e4m3 take 108
 // us: 1.6 TB/s, 340 TFLOP/s.
@@ -1323,13 +1324,25 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
                 to[t] = T::mfma(operand(x, width), q[i / W::kSTiles], to[t]);
             });
     };
+    // Where a lane's four values of each 32 columns are, in a tile's first 16 keys
+    // (rows 16 apart are permuted alike).  Sums that the compiler takes apart
+    // grow into chains whose array it no longer knows, and a read of that waits
+    // for everything on its way to LDS.
+    uint32_t value_at[W::kDTiles];
+#pragma unroll
+    for (uint32_t dt = 0; dt < W::kDTiles; ++dt) {
+        const uint32_t g = lane & 15u, r = 4 * hi + (g >> 2), d = 32 * dt + (lane & 16u) + 4 * (g & 3u);
+        value_at[dt] = (r * W::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2;
+        asm volatile("" : "+v"(value_at[dt]));
+    }
     // adds a tile's values by their weights
     auto add = [&](const uint8_t* __restrict__ values, uint32_t (*p)[8], auto width) __attribute__((always_inline)) {
         const uint32_t g = lane & 15u;
         products<2 * W::kSTiles * W::kDTiles>(
             [&](uint32_t i) -> u32x4 {
-                const uint32_t dt = i % W::kDTiles, r0 = 16 * (i / W::kDTiles) + 4 * hi;
+                const uint32_t dt = i % W::kDTiles;
                 if constexpr (decltype(width)::value) {
+                    const uint32_t r0 = 16 * (i / W::kDTiles) + 4 * hi;
                     // eight rows of 16 columns: keys 0..3 and 8..11 of the lane's half
                     typedef int i32x2 __attribute__((ext_vector_type(2)));
                     typedef __attribute__((address_space(3))) i32x2 Two;
@@ -1339,8 +1352,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
                     return {static_cast<uint32_t>(x[0]), static_cast<uint32_t>(x[1]), 0, 0};
                 } else {
                     typedef __attribute__((address_space(3))) s16x4 Four;
-                    const uint32_t r = r0 + (g >> 2), d = 32 * dt + (lane & 16u) + 4 * (g & 3u);
-                    const uint8_t* const at = values + (r * W::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2;
+                    const uint8_t* const at = values + (value_at[dt] + 16 * (i / W::kDTiles) * kDim * 2);
                     const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four*)at);
                     // (rows eight apart are permuted alike)
                     const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Four*)(at + 8 * kDim * 2));
