@@ -337,7 +337,8 @@ class TreeAttention(_Call):
     piece of one; single tokens).  A parent that is neither -1 nor an earlier
     token makes its token void: a zero row, which no other token sees.
     scale: of the products, dim ** -0.5 by default.  Result: `out` [tokens,
-    q_heads, dim] of q's type."""
+    q_heads, dim] of q's type; rows past token_offsets[requests] (a padded
+    batch) are not written."""
 
     def __init__(self, q, k, v, k_cache, v_cache, table, lengths, token_offsets, parents=None, *,
                  scale: Optional[float] = None, k_scale=None, v_scale=None,
@@ -363,7 +364,7 @@ class TreeAttention(_Call):
             _vector(parents, "parents", torch.int32, device, n)
         made = []
         if out is None:
-            out = torch.empty((n, q_heads, dim), dtype=q.dtype, device=device)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
             made.append(out)
         else:
             _vector(out, "out", q.dtype, device, n, q_heads, dim)
