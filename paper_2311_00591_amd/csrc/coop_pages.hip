@@ -618,11 +618,13 @@ Divide divide_by(uint32_t d) {
 
 // x / scale.  For scales of ordinary size, `inverse` is 1 / scale and the
 // product with it is corrected by its remainder, which gives the rounded
-// quotient; a quotient of 512 or more ends at the largest number anyway.
+// quotient; a quotient of 512 or more ends at the largest number anyway.  The
+// remainder of a zero, or of what the correction takes to zero, has a sign of
+// its own: the quotient's is the product's.
 __device__ __forceinline__ float quotient(float x, float scale, float inverse, bool ordinary) {
     if (!ordinary) return x / scale;
     const float y = x * inverse;
-    return fabsf(y) >= 512.f ? y : fmaf(fmaf(-y, scale, x), inverse, y);
+    return fabsf(y) >= 512.f ? y : copysignf(fmaf(fmaf(-y, scale, x), inverse, y), y);
 }
 
 // Pairs of numbers in e4m3, limited to its largest value; NaN stays NaN.
