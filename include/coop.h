@@ -474,7 +474,8 @@ coop_status_t coop_cache_write(const coop_rows_t *k, const coop_rows_t *v, int32
  *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j
  * over the tokens j that t sees.  Products have 16-bit operands and 32-bit
  * sums; the softmax's statistics are 32-bit; its weights are rounded to `type`
- * before they meet the values.
+ * before they meet the values (in COOP_FP16, those below 2^-21 of the largest by
+ * a fixed step, 2^-31 of it).
  *
  * q, k_new, v_new, out: `type` (COOP_BF16 or COOP_FP16); the cache has the
  * same type or COOP_E4M3.  q_heads is a multiple of cache->heads.  out

@@ -63,7 +63,7 @@ constexpr uint32_t kParentsInLds = 512;   // trees up to this size are walked in
 constexpr uint32_t kPlanThreads = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLowest = -__builtin_inff();
-constexpr float kSlack = 8.f;  // how far, in powers of two, scores may pass the sums' base
+constexpr float kSlack = 8.f;  // how far, in powers of two, the largest weight may grow
 
 struct Item {  // rows [32 kRowWaves rt, ...) of a request and head, tiles [first, last)
     uint32_t request, row_tile, head, first, last;
@@ -428,6 +428,7 @@ struct Bf16 {
     typedef __bf16 Vec8 __attribute__((ext_vector_type(8)));
     typedef __bf16 Vec2 __attribute__((ext_vector_type(2)));
     static constexpr uint32_t kExponent = 0x7f80u;
+    static constexpr float kLift = 0.f;  // the largest weight is taken as 2^kLift
     static __device__ __forceinline__ f32x16 mfma(u32x4 x, u32x4 y, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(Vec8, x),
                                                        __builtin_bit_cast(Vec8, y), c, 0, 0, 0);
@@ -450,6 +451,11 @@ struct Fp16 {
     typedef _Float16 Vec8 __attribute__((ext_vector_type(8)));
     typedef _Float16 Vec2 __attribute__((ext_vector_type(2)));
     static constexpr uint32_t kExponent = 0x7c00u;
+    // Numbers below 2^-14 have a fixed step of 2^-24, which a sum of many small
+    // weights would feel (a first token with a score far above all others).
+    // Lifted, weights are at most 2^(kLift + kSlack) = 2^15, which fp16 holds,
+    // and lose bits only from 2^-21 of the largest down.
+    static constexpr float kLift = 7.f;
     static __device__ __forceinline__ f32x16 mfma(u32x4 x, u32x4 y, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(Vec8, x),
                                                       __builtin_bit_cast(Vec8, y), c, 0, 0, 0);
@@ -612,12 +618,12 @@ __device__ __forceinline__ bool take_item(const Args& a, Item* item, Extent* e) 
 
 // Masks the scores of a tile and moves the sums' base.  Scores are s * factor;
 // where keys are masked, or the factor is negative and does not keep the
-// maximum, they are formed here, and the factor becomes one.  The base stays
-// until a score passes it by kSlack: weights are then at most 2^kSlack, which
-// every type here holds, and the accumulators are seldom scaled (l and o have
-// a common factor that the division takes out).  Returns what o is to be
-// multiplied by.
-template <uint32_t kTiles>
+// maximum, they are formed here, and the factor becomes one.  The base is
+// T::kLift below the largest score, and stays until a weight passes 2^kLift by
+// 2^kSlack: weights are then at most 2^(kLift + kSlack), which the type holds,
+// and the accumulators are seldom scaled (l and o have a common factor that the
+// division takes out).  Returns what o is to be multiplied by.
+template <class T, uint32_t kTiles>
 __device__ __forceinline__ float new_base(f32x16* s, uint64_t sees, uint64_t full, uint32_t hi,
                                           float* factor, float* m, float* l) {
     if (*factor < 0.f || !__all(sees == full)) {
@@ -635,7 +641,7 @@ __device__ __forceinline__ float new_base(f32x16* s, uint64_t sees, uint64_t ful
     for (uint32_t t = 0; t < kTiles; ++t)
 #pragma unroll
         for (uint32_t i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-    top = fmaxf(top, __shfl_xor(top, 32, 64)) * *factor;
+    top = fmaxf(top, __shfl_xor(top, 32, 64)) * *factor - T::kLift;
     float grow = 1.f;
     if (__any(top > *m + kSlack)) {
         const float m2 = fmaxf(*m, top);
@@ -966,7 +972,7 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
             if (is_new)
                 sees = sight.of_tile<kKeys>(static_cast<int32_t>((cached_tiles + new_tiles - 1 - tile) * kKeys));
             float factor = is_new ? new_scale : cached_scale;
-            float grow = new_base<S::kSTiles>(s, sees, kFull, hi, &factor, &m, &l);
+            float grow = new_base<T, S::kSTiles>(s, sees, kFull, hi, &factor, &m, &l);
             uint32_t p[S::kSTiles][8];
             l += weights_of<T, S::kSTiles>(s, factor, m, p);
             if (kE4M3 && is_new && !scaled) {
@@ -1371,7 +1377,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
         uint64_t sees = counts;
         if (is_new) sees = sight.of_tile<kKeys>(static_cast<int32_t>((all_tiles - 1 - tile) * kKeys));
         float factor = is_new ? new_scale : cached_scale;
-        float grow = new_base<W::kSTiles>(s, sees, kFull, hi, &factor, &m, &l);
+        float grow = new_base<T, W::kSTiles>(s, sees, kFull, hi, &factor, &m, &l);
         if (kNew && !scaled) {
             grow *= value_scale;
             scaled = true;
