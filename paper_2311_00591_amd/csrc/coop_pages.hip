@@ -619,12 +619,15 @@ Divide divide_by(uint32_t d) {
 // x / scale.  For scales of ordinary size, `inverse` is 1 / scale and the
 // product with it is corrected by its remainder, which gives the rounded
 // quotient; a quotient of 512 or more ends at the largest number anyway.  The
-// remainder of a zero, or of what the correction takes to zero, has a sign of
-// its own: the quotient's is the product's.
+// remainder is taken with the sign that keeps a zero's: y scale - x is plus zero
+// for either zero x, and what is added to y then is minus zero.  (Ordinary
+// scales are above zero, and none takes a number other than zero to zero: the
+// least is 2^-133 over 2^15, twice the 32-bit step, and the product is off by
+// one step at most.)
 __device__ __forceinline__ float quotient(float x, float scale, float inverse, bool ordinary) {
     if (!ordinary) return x / scale;
     const float y = x * inverse;
-    return fabsf(y) >= 512.f ? y : copysignf(fmaf(fmaf(-y, scale, x), inverse, y), y);
+    return fabsf(y) >= 512.f ? y : fmaf(-fmaf(y, scale, -x), inverse, y);
 }
 
 // Pairs of numbers in e4m3, limited to its largest value; NaN stays NaN.
@@ -682,7 +685,7 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(WriteArgs a) {
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
                 const float scale = (side ? cache.v_scale : cache.k_scale)[h], inverse = 1.f / scale;
-                const bool ordinary = fabsf(scale) >= 0x1p-60f && fabsf(scale) <= 0x1p60f &&
+                const bool ordinary = scale >= 0x1p-60f && scale <= 0x1p15f &&
                                       (~__float_as_uint(scale) & 0x7fffffu) != 0;
                 const uint4 x = side ? vx : kx;
                 const uint32_t word[4] = {x.x, x.y, x.z, x.w};

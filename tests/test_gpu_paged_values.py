@@ -24,12 +24,12 @@ def _announce(label):
 @pytest.mark.parametrize("dtype", [BF16, FP16])
 def test_cache_write_stores_the_quotients_bytes(dtype):
     """Byte for byte x / scale in 32 bits, limited and rounded: signed zeros,
-    numbers that come to zero, and scales past the usual sizes (2^-60 to 2^60,
-    a mantissa that is not all ones), which are divided by another way."""
+    numbers that come to zero, and scales past the usual ones (2^-60 to 2^15, a
+    mantissa that is not all ones), which are divided by another way."""
     coop = _coop()
     _announce(f"write, bytes of quotients, {dtype}")
     scales = torch.tensor([1.0, 0.013, -0.5, 2.0**-60, 2.0**60, 2.0**-61, 2.0**61, 2.0**-70,
-                           2.0**70, 2.0 - 2.0**-23, 2.0**-100, 3.0e38])
+                           2.0**70, 2.0 - 2.0**-23, 2.0**-100, 3.0e38, 2.0**15, 32767.0, 3.0, 2.0**17])
     heads, dim, tokens = len(scales), 64, 40
     g = torch.Generator().manual_seed(3)
     # numbers around what e4m3 holds, times the scale, where the type reaches that far
