@@ -21,7 +21,6 @@ import functools
 from typing import Optional
 
 import torch
-from torch._C import _cuda_getCurrentRawStream as _current_stream, _cuda_getDevice as _current_device
 
 from . import COOP_EVICTABLE, COOP_PINNED, _check, _ptr, load_library
 
@@ -40,6 +39,11 @@ class CoopCache(ctypes.Structure):
 class CoopRows(ctypes.Structure):
     """coop_rows_t."""
     _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_uint64 * 2)]
+
+
+def _current_stream(index: int) -> int:
+    # (torch without GPU support lacks the name, so it is looked up by the call)
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _gpu(device):
@@ -152,7 +156,7 @@ class _Call:
             other = torch.cuda.ExternalStream(stream, self.device)
             for t in self._made:
                 t.record_stream(other)
-        if _current_device() == index:
+        if torch._C._cuda_getDevice() == index:
             status = self._fn(*self._args, stream)
         else:
             with torch.cuda.device(self.device):
