@@ -46,6 +46,11 @@ def _current_stream(index: int) -> int:
     return torch._C._cuda_getCurrentRawStream(index)
 
 
+def _stream(handle: int, device):
+    # (ExternalStream takes 0 for no stream and makes one)
+    return torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
+
+
 def _gpu(device):
     if device.type != "cuda":
         raise ValueError(f"paged pools are worked on by the GPU; tensors are on {device} "
@@ -153,7 +158,7 @@ class _Call:
             stream = current
         elif stream != current:
             # memory from torch's allocator is not reused before that stream is done with it
-            other = torch.cuda.ExternalStream(stream, self.device)
+            other = _stream(stream, self.device)
             for t in self._made:
                 t.record_stream(other)
         if torch._C._cuda_getDevice() == index:

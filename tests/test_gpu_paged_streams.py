@@ -1,0 +1,91 @@
+"""Paged-pool calls on other streams than the one that they were made on."""
+import sys
+import time
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+DEV = "cuda"
+
+
+def _coop():
+    import paper_2311_00591_amd as coop
+    return coop
+
+
+def _announce(label):
+    print(f"[gpu case] paged: {label}", flush=True)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def busy():
+    """Enqueues some 50 ms of products on the current stream; returns an event
+    behind them."""
+    a = torch.zeros((8192, 8192), dtype=BF16, device=DEV)
+    out = torch.empty_like(a)
+    torch.mm(a, a, out=out)
+    torch.cuda.synchronize()
+
+    def enqueue(n=60):
+        for _ in range(n):
+            torch.mm(a, a, out=out)
+        return torch.cuda.current_stream().record_event()
+
+    start = time.perf_counter()
+    enqueue(20).synchronize()
+    took = (time.perf_counter() - start) / 20
+    return lambda: enqueue(int(0.05 / took) + 1)
+
+
+def _attention():
+    g = torch.Generator(device=DEV).manual_seed(1)
+    rnd = lambda *s: torch.randn(s, generator=g, device=DEV, dtype=BF16)
+    return dict(q=rnd(8, 8, 128), k=rnd(8, 2, 128), v=rnd(8, 2, 128), k_cache=rnd(40, 16, 2, 128),
+                v_cache=rnd(40, 16, 2, 128),
+                table=torch.randperm(40, generator=g, device=DEV).to(torch.int32).view(2, 20),
+                lengths=torch.tensor([300, 77], device=DEV),
+                token_offsets=torch.tensor([0, 3, 8], device=DEV))
+
+
+def _memory_of(t):
+    return t.data_ptr(), t.untyped_storage().nbytes()
+
+
+def _taken_while(event, memory):
+    """Allocates and overwrites as much as `memory` says, many times over, on
+    the current stream; whether any of it was that memory, and whether `event`
+    was still ahead."""
+    hit = []
+    for at, size in memory:
+        for t in [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(4)]:
+            t.fill_(0xff)
+            hit.append(t.data_ptr() < at + size and at < t.data_ptr() + size)
+    return any(hit), not event.query()
+
+
+def test_the_default_stream_by_its_handle(busy):
+    """stream=0 names the default stream, while another one is current: memory
+    of a dropped call is not handed out before the default stream is done."""
+    coop = _coop()
+    _announce("the default stream's handle")
+    a = _attention()
+    want = coop.tree_attention(**a)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    copy = torch.empty_like(want)
+    ahead = busy()
+    with torch.cuda.stream(side):
+        call = coop.TreeAttention(**a)
+        call.launch(torch.cuda.default_stream().cuda_stream)
+        memory = [_memory_of(call.out), _memory_of(call.workspace)]
+        with torch.cuda.stream(torch.cuda.default_stream()):
+            copy.copy_(call.out)
+        del call
+        taken, waiting = _taken_while(ahead, memory)
+    assert waiting and not taken
+    torch.cuda.synchronize()
+    assert torch.equal(copy, want)
