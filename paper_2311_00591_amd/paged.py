@@ -141,26 +141,50 @@ def _workspace(workspace: Optional[torch.Tensor], need: int, device, made):
     return workspace, workspace.data_ptr(), held
 
 
+def _capturing(stream) -> bool:
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class _Call:
     """A prepared call: the C function, its arguments (all but the stream) and
     the tensors that it uses, which it keeps alive.  `made` are those that it
-    allocated itself."""
+    allocated itself, on the stream that is current now."""
+
+    _met = ()  # the other streams that the call was launched on
 
     def _prepare(self, device, fn, args, made):
         self.device, self._fn, self._args, self._made = device, fn, args, made
+        self._home = _current_stream(device.index)
+
+    def _meet(self, stream: int) -> None:
+        """Puts `stream` behind what is queued on the call's own stream, where
+        the memory that it allocated may still be in use from before, and keeps
+        that memory from being handed out again before `stream` is done."""
+        other = _stream(stream, self.device)
+        home = _stream(self._home, self.device)
+        if _capturing(other) or torch.cuda.is_current_stream_capturing():
+            # a graph cannot wait for what is outside of it, and its owner keeps the call
+            # (the default stream, 0, is never captured)
+            if not (self._home and _capturing(home)):
+                return
+        other.wait_stream(home)
+        for t in self._made:
+            t.record_stream(other)
+        self._met += (stream,)
 
     def launch(self, stream: Optional[int] = None) -> None:
         """Enqueues the call on `stream` (default: torch's current stream of
-        the tensors' device)."""
+        the tensors' device).  The first launch on another stream than the one
+        that was current when the call was made waits for what is queued there
+        by then; apart from that, the inputs are to be ready on `stream`, and
+        launches, which share results and workspace, in order.  A call that a
+        graph captured is to be kept as long as the graph."""
         index = self.device.index
-        current = _current_stream(index)
         if stream is None:
-            stream = current
-        elif stream != current:
-            # memory from torch's allocator is not reused before that stream is done with it
-            other = _stream(stream, self.device)
-            for t in self._made:
-                t.record_stream(other)
+            stream = _current_stream(index)
+        if stream != self._home and stream not in self._met:
+            self._meet(stream)
         if torch._C._cuda_getDevice() == index:
             status = self._fn(*self._args, stream)
         else:

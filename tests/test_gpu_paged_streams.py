@@ -89,3 +89,114 @@ def test_the_default_stream_by_its_handle(busy):
     assert waiting and not taken
     torch.cuda.synchronize()
     assert torch.equal(copy, want)
+
+
+def test_memory_is_waited_for(busy):
+    """Results and workspaces come from the allocator for the stream that is
+    current, where work on what was there before may be under way: a call on
+    another stream starts behind it, a later launch there does not wait again."""
+    coop = _coop()
+    _announce("other streams wait for the memory")
+    a = _attention()
+    want = coop.tree_attention(**a)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    ahead = busy()
+    got = coop.tree_attention(**a, stream=side.cuda_stream)
+    done = side.record_event()
+    time.sleep(0.01)
+    early = done.query()
+    assert not ahead.query() and not early
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+    call = coop.TreeAttention(**a)
+    call.launch()
+    torch.cuda.synchronize()
+    call.out.zero_()
+    ahead = busy()
+    with torch.cuda.stream(side):
+        call.launch()
+    done = side.record_event()
+    time.sleep(0.01)
+    early = done.query()
+    assert not ahead.query() and not early
+    torch.cuda.synchronize()
+    assert torch.equal(call.out, want)
+
+    call.out.zero_()
+    torch.cuda.synchronize()
+    ahead = busy()
+    call.launch(side.cuda_stream)
+    side.record_event().synchronize()
+    assert not ahead.query()
+    torch.cuda.synchronize()
+    assert torch.equal(call.out, want)
+
+
+def test_memory_is_kept_for_the_stream_that_uses_it(busy):
+    """A call made on one stream, launched while another is current and
+    dropped: its memory is not handed out before that stream is done."""
+    coop = _coop()
+    _announce("memory kept for another stream")
+    a = _attention()
+    want = coop.tree_attention(**a)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    copy = torch.empty_like(want)
+    call = coop.TreeAttention(**a)
+    memory = [_memory_of(call.out), _memory_of(call.workspace)]
+    with torch.cuda.stream(side):
+        ahead = busy()
+        call.launch()
+        copy.copy_(call.out)
+    del call
+    taken, waiting = _taken_while(ahead, memory)
+    assert waiting and not taken
+    torch.cuda.synchronize()
+    assert torch.equal(copy, want)
+
+
+def test_prepared_calls_are_captured_on_another_stream():
+    """A call made before the capture, on the stream that was current then."""
+    coop = _coop()
+    _announce("a prepared call captured")
+    a = _attention()
+    want = coop.tree_attention(**a)
+    call = coop.TreeAttention(**a)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call.launch()
+    for _ in range(4):
+        call.out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(call.out, want)
+        assert torch.equal(coop.tree_attention(**a), want)
+    # and eagerly on a third one afterwards
+    side = torch.cuda.Stream()
+    call.out.zero_()
+    call.launch(side.cuda_stream)
+    torch.cuda.synchronize()
+    assert torch.equal(call.out, want)
+
+
+def test_a_branch_of_a_capture():
+    """A call on a second stream of the capture, which the first one joins."""
+    coop = _coop()
+    _announce("a branch of a capture")
+    a = _attention()
+    want = coop.tree_attention(**a)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = coop.tree_attention(**a, stream=side.cuda_stream)
+        torch.cuda.current_stream().wait_stream(side)
+        twice = got + got
+    for _ in range(4):
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(twice, want + want)
