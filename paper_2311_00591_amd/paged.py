@@ -6,7 +6,9 @@ first_fit read, so they work on it too.  As in the rest of the package, every
 step runs in the HIP kernels of libcoop.so, calls are asynchronous on torch's
 current stream (or the `stream` argument), and each operator comes as a
 prepared call (a class whose `launch` can be repeated or captured into a graph)
-and as a function.
+and as a function.  A function called with `stream` runs behind what is queued
+on the current stream; its inputs may be dropped at once, its results are there
+when `stream` is done.
 
 Caches are tensors [pages, page_size, heads, dim] of bfloat16, float16 or
 float8_e4m3fn, in any order of the first three dimensions in memory (a
@@ -125,13 +127,12 @@ def _cache(k_cache, v_cache, k_scale, v_scale, dtype, device) -> CoopCache:
                      _TYPES[kind])
 
 
-def _workspace(workspace: Optional[torch.Tensor], need: int, device, made):
+def _workspace(workspace: Optional[torch.Tensor], need: int, device):
     """(the workspace to keep alive, its address, its bytes)."""
     if workspace is None:
         if need == 0:
             return None, None, 0
         workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        made.append(workspace)
         return workspace, workspace.data_ptr(), need
     if workspace.device != device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be contiguous memory on {device}")
@@ -148,19 +149,20 @@ def _capturing(stream) -> bool:
 
 class _Call:
     """A prepared call: the C function, its arguments (all but the stream) and
-    the tensors that it uses, which it keeps alive.  `made` are those that it
-    allocated itself, on the stream that is current now."""
+    the tensors that it uses (None where there is none), which it keeps alive."""
 
     _met = ()  # the other streams that the call was launched on
 
-    def _prepare(self, device, fn, args, made):
-        self.device, self._fn, self._args, self._made = device, fn, args, made
+    def _prepare(self, device, fn, args, tensors):
+        self.device, self._fn, self._args, self._tensors = device, fn, args, tensors
         self._home = _current_stream(device.index)
 
     def _meet(self, stream: int) -> None:
-        """Puts `stream` behind what is queued on the call's own stream, where
-        the memory that it allocated may still be in use from before, and keeps
-        that memory from being handed out again before `stream` is done."""
+        """Puts `stream` behind what is queued on the stream that the call was
+        made on, where the memory that it allocated may still be in use from
+        before, and keeps all of its tensors' memory (inputs may be dropped as
+        soon as the call is) from being handed out again before `stream` is
+        done."""
         other = _stream(stream, self.device)
         home = _stream(self._home, self.device)
         if _capturing(other) or torch.cuda.is_current_stream_capturing():
@@ -169,8 +171,9 @@ class _Call:
             if not (self._home and _capturing(home)):
                 return
         other.wait_stream(home)
-        for t in self._made:
-            t.record_stream(other)
+        for t in self._tensors:
+            if t is not None:
+                t.record_stream(other)
         self._met += (stream,)
 
     def launch(self, stream: Optional[int] = None) -> None:
@@ -237,23 +240,21 @@ class PageTables(_Call):
             raise ValueError(f"taken must be COOP_EVICTABLE or COOP_PINNED, got {taken}")
         if out is None:
             out = (torch.empty_like(table), torch.empty_like(held), torch.empty_like(kind))
-            made = list(out)
         else:
-            made = []
             _vector(out[0], "out[0]", torch.int32, device, rows, cols)
             _vector(out[1], "out[1]", torch.int32, device, rows)
             _vector(out[2], "out[2]", torch.uint8, device, pages)
         self.table, self.held, self.kind = out
         self.status = torch.empty(1, dtype=torch.int32, device=device)
         self.free = torch.empty(1, dtype=torch.int64, device=device)
-        made += (self.status, self.free)
         self.workspace, ws, ws_bytes = _workspace(
-            workspace, page_tables_workspace_size(pages, rows), device, made)
-        self._inputs = (kind, table, held, lengths)
+            workspace, page_tables_workspace_size(pages, rows), device)
         self._prepare(device, load_library().coop_page_tables,
                       (_ptr(kind), pages, _ptr(table), rows, cols, _ptr(held), _ptr(lengths),
                        page_size, taken, _ptr(self.table), _ptr(self.held), _ptr(self.kind),
-                       self.status.data_ptr(), self.free.data_ptr(), ws, ws_bytes), made)
+                       self.status.data_ptr(), self.free.data_ptr(), ws, ws_bytes),
+                      (kind, table, held, lengths, self.table, self.held, self.kind, self.status,
+                       self.free, self.workspace))
 
     def __call__(self, stream: Optional[int] = None):
         self.launch(stream)
@@ -287,16 +288,13 @@ class SlotMap(_Call):
         if num_tokens < 0 or page_size < 1 or num_pages < 0:
             raise ValueError(f"num_tokens {num_tokens}, page_size {page_size} and num_pages "
                              f"{num_pages} must be at least 0, 1 and 0")
-        made = []
         if out is None:
             out = torch.empty(num_tokens, dtype=torch.int64, device=device)
-            made = [out]
         self.slots = _vector(out, "out", torch.int64, device, num_tokens)
-        self._inputs = (table, held, lengths, token_offsets)
         self._prepare(device, load_library().coop_slot_map,
                       (_ptr(table), rows, cols, _ptr(held), _ptr(lengths),
                        token_offsets.data_ptr(), num_tokens, page_size, num_pages,
-                       _ptr(self.slots)), made)
+                       _ptr(self.slots)), (table, held, lengths, token_offsets, self.slots))
 
     def __call__(self, stream: Optional[int] = None) -> torch.Tensor:
         self.launch(stream)
@@ -329,10 +327,9 @@ class CacheWrite(_Call):
         v_rows = _rows(v, "v", k.dtype, device, shape)
         _vector(slots, "slots", torch.int64, device, n)
         self.k_cache, self.v_cache = k_cache, v_cache
-        self._inputs = (k, v, slots, k_scale, v_scale)
         self._prepare(device, load_library().coop_cache_write,
                       (ctypes.byref(k_rows), ctypes.byref(v_rows), _TYPES[k.dtype], _ptr(slots), n,
-                       ctypes.byref(cache)), [])
+                       ctypes.byref(cache)), (k, v, slots, k_cache, v_cache, k_scale, v_scale))
 
     def __call__(self, stream: Optional[int] = None):
         self.launch(stream)
@@ -395,25 +392,22 @@ class TreeAttention(_Call):
         _vector(token_offsets, "token_offsets", torch.int64, device, requests + 1)
         if parents is not None:
             _vector(parents, "parents", torch.int32, device, n)
-        made = []
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
-            made.append(out)
         else:
             _vector(out, "out", q.dtype, device, n, q_heads, dim)
         self.out = out
         self.workspace, ws, ws_bytes = _workspace(
             workspace, tree_attention_workspace_size(requests, n, q_heads, cache.heads, dim),
-            device, made)
-        self._inputs = (q, k, v, k_cache, v_cache, table, lengths, token_offsets, parents, k_scale,
-                        v_scale)
+            device)
         self._prepare(device, load_library().coop_tree_attention,
                       (ctypes.byref(q_rows), ctypes.byref(k_rows), ctypes.byref(v_rows),
                        _TYPES[q.dtype], q_heads, n, token_offsets.data_ptr(),
                        None if parents is None else _ptr(parents), ctypes.byref(cache), _ptr(table),
                        cols, _ptr(lengths), requests,
                        dim ** -0.5 if scale is None else float(scale), _ptr(out), ws, ws_bytes),
-                      made)
+                      (q, k, v, k_cache, v_cache, table, lengths, token_offsets, parents, k_scale,
+                       v_scale, out, self.workspace))
 
     def __call__(self, stream: Optional[int] = None) -> torch.Tensor:
         self.launch(stream)

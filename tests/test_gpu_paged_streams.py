@@ -200,3 +200,28 @@ def test_a_branch_of_a_capture():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(twice, want + want)
+
+
+def test_inputs_are_kept_for_the_stream_that_reads_them(busy):
+    """Inputs that are dropped with the call, made for it alone (accepted
+    tokens' rows): their memory is not handed out before they were read."""
+    coop = _coop()
+    _announce("inputs kept for another stream")
+    g = torch.Generator(device=DEV).manual_seed(2)
+    k, v = (torch.randn((64, 8, 128), generator=g, device=DEV, dtype=BF16) for _ in "kv")
+    k_cache, v_cache = (torch.zeros((8, 16, 8, 128), device=DEV, dtype=BF16) for _ in "kv")
+    picked = torch.randperm(64, generator=g, device=DEV)
+    slots = torch.arange(64, device=DEV)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        ahead = busy()
+    rows = [k[picked], v[picked], slots + 64]
+    memory = [_memory_of(t) for t in rows]
+    coop.cache_write(*rows, k_cache, v_cache, stream=side.cuda_stream)
+    del rows
+    taken, waiting = _taken_while(ahead, memory)
+    assert waiting and not taken
+    torch.cuda.synchronize()
+    for cache, x in ((k_cache, k), (v_cache, v)):
+        assert torch.equal(cache.view(128, 8, 128)[64:], x[picked]) and not cache[:4].any()
