@@ -420,7 +420,8 @@ typedef enum {
  * multiples of 16 bytes; dim is a multiple of 8 (of 16 with COOP_E4M3) and at
  * most 256.  With COOP_E4M3 an element stands for its value times
  * k_scale[head] or v_scale[head] (device); otherwise both are NULL.  num_pages
- * and page_size are at most 2^31 - 1. */
+ * and page_size are at most 2^31 - 1, a stride at most 2^40, and the last
+ * element is less than 2^60 elements from the first. */
 typedef struct {
     void *k;
     void *v;

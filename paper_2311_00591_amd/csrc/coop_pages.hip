@@ -850,7 +850,8 @@ coop_status_t coop_cache_write(const coop_rows_t* k, const coop_rows_t* v, int32
     if (const coop_status_t rc = coop_pages::check_cache(*cache, type)) return rc;
     if (num_tokens == 0 || cache->num_pages == 0) return COOP_OK;
     if (!slots || num_tokens > (1ull << 40)) return COOP_ERR_INVALID;
-    if (!coop_pages::rows_valid(*k, num_tokens) || !coop_pages::rows_valid(*v, num_tokens))
+    if (!coop_pages::rows_valid(*k, num_tokens, cache->heads, cache->dim) ||
+        !coop_pages::rows_valid(*v, num_tokens, cache->heads, cache->dim))
         return COOP_ERR_INVALID;
     WriteArgs a;
     a.k = *k;

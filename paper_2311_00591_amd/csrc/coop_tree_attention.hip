@@ -1657,8 +1657,9 @@ coop_status_t coop_tree_attention(const coop_rows_t* q, const coop_rows_t* k_new
         max_pages > kMost || max_pages * cache->page_size > kMost)
         return COOP_ERR_INVALID;
     if (num_tokens == 0) return COOP_OK;
-    if (!coop_pages::rows_valid(*q, num_tokens) || !coop_pages::rows_valid(*k_new, num_tokens) ||
-        !coop_pages::rows_valid(*v_new, num_tokens))
+    if (!coop_pages::rows_valid(*q, num_tokens, q_heads, cache->dim) ||
+        !coop_pages::rows_valid(*k_new, num_tokens, cache->heads, cache->dim) ||
+        !coop_pages::rows_valid(*v_new, num_tokens, cache->heads, cache->dim))
         return COOP_ERR_INVALID;
     if (!out || !coop_pages::aligned16(out) || !token_offsets) return COOP_ERR_INVALID;
     if (num_requests == 0) return COOP_OK;
