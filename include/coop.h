@@ -359,7 +359,8 @@ coop_status_t coop_replay(uint64_t *size, uint64_t *cost, uint8_t *kind, uint32_
  * above that range) and lengths[] (device: the tokens each sequence is to
  * hold) are read; table_out, held_out and kind_out are written.  Each of the
  * three may be its input (the update is then in place) or must not overlap
- * any input.  A page is in one row at most.
+ * any input, and no output or workspace overlaps another.  A page is in one row
+ * at most.
  *
  * A sequence of n tokens needs ceil(n / page_size) pages.
  *  1. Rows that hold more than they need give back their last pages: these
@@ -399,7 +400,7 @@ coop_status_t coop_page_tables(const uint8_t *kind, uint64_t num_pages, const in
  * page_size for the token at position pos, and -1 where there is no such
  * place: the entry is at or past held[b], its page is not below num_pages,
  * the sequence has more new tokens than it has tokens, or the token lies past
- * token_offsets[num_requests].
+ * token_offsets[num_requests].  slots must not overlap what is read.
  */
 coop_status_t coop_slot_map(const int32_t *table, uint64_t num_requests, uint64_t max_pages,
                             const int32_t *held, const uint64_t *lengths,

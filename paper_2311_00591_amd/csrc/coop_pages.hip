@@ -737,10 +737,15 @@ TablesLayout tables_layout(uint64_t pages, uint64_t rows) {
     return l;
 }
 
-// Whether [a, a + na) and [b, b + nb) share a byte.
-bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return na && nb && x < y + nb && y < x + na;
+struct Span {
+    const void* at;
+    uint64_t bytes;
+};
+
+// Whether two arrays share a byte.
+bool overlap(const Span& a, const Span& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+    return a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
 }
 
 }  // namespace
@@ -767,18 +772,20 @@ coop_status_t coop_page_tables(const uint8_t* kind, uint64_t num_pages, const in
     if (num_requests && (!held || !lengths || !held_out)) return COOP_ERR_INVALID;
     if (num_requests && max_pages && (!table || !table_out)) return COOP_ERR_INVALID;
     if (!status || !free_pages) return COOP_ERR_INVALID;
-    {   // an output is its input or apart from every input
-        const uint64_t tb = num_requests * max_pages * 4, hb = num_requests * 4, nb = num_requests * 8;
-        const struct { const void* out; uint64_t bytes; const void* in; } outs[3] = {
-            {table_out, tb, table}, {held_out, hb, held}, {kind_out, num_pages, kind}};
-        const struct { const void* in; uint64_t bytes; } ins[4] = {
-            {table, tb}, {held, hb}, {kind, num_pages}, {lengths, nb}};
-        for (const auto& o : outs)
-            for (const auto& i : ins)
-                if (!(o.in == i.in && o.out == o.in) && overlap(o.out, o.bytes, i.in, i.bytes))
-                    return COOP_ERR_INVALID;
-    }
     const TablesLayout l = tables_layout(num_pages, num_requests);
+    {   // an output is its input or apart from every input, and from the others
+        const uint64_t tb = num_requests * max_pages * 4, hb = num_requests * 4, nb = num_requests * 8;
+        const Span in[4] = {{table, tb}, {held, hb}, {kind, num_pages}, {lengths, nb}};
+        const Span out[6] = {{table_out, tb}, {held_out, hb}, {kind_out, num_pages},
+                             {status, sizeof(*status)}, {free_pages, sizeof(*free_pages)},
+                             {workspace, workspace ? l.bytes : 0}};
+        for (int o = 0; o < 6; ++o) {
+            for (int i = 0; i < 4; ++i)
+                if (!(o == i && i < 3 && out[o].at == in[i].at) && overlap(out[o], in[i])) return COOP_ERR_INVALID;
+            for (int i = 0; i < o; ++i)
+                if (overlap(out[o], out[i])) return COOP_ERR_INVALID;
+        }
+    }
     if (l.bytes && (!workspace || workspace_bytes < l.bytes)) return COOP_ERR_WORKSPACE;
     if (l.bytes && !coop_pages::aligned16(workspace)) return COOP_ERR_INVALID;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -836,6 +843,12 @@ coop_status_t coop_slot_map(const int32_t* table, uint64_t num_requests, uint64_
     if (!slots || !token_offsets) return COOP_ERR_INVALID;
     if (num_requests && (!held || !lengths)) return COOP_ERR_INVALID;
     if (num_requests && max_pages && !table) return COOP_ERR_INVALID;
+    const Span out = {slots, num_tokens * sizeof(*slots)};
+    for (const Span& in : {Span{table, num_requests * max_pages * sizeof(*table)},
+                           Span{held, num_requests * sizeof(*held)},
+                           Span{lengths, num_requests * sizeof(*lengths)},
+                           Span{token_offsets, (num_requests + 1) * sizeof(*token_offsets)}})
+        if (overlap(out, in)) return COOP_ERR_INVALID;
     hipLaunchKernelGGL(slot_map_kernel, dim3(grid_for(num_tokens, kThreads / 64 * kWaveTokens)), dim3(kThreads), 0,
                        static_cast<hipStream_t>(stream), table, static_cast<uint32_t>(num_requests),
                        static_cast<uint32_t>(max_pages), held, lengths, token_offsets, num_tokens,

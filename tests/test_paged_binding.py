@@ -69,3 +69,41 @@ def test_a_dimension_of_one_may_have_any_stride():
     one = _cache_of(num_pages=1, page_size=1, heads=1, k_stride=(1 << 40,) * 3, v_stride=(1 << 40,) * 3)
     rows = CoopRows(NZ, (1 << 40, 1 << 40))
     assert lib.coop_cache_write(rows, rows, 0, NZ, 0, one, None) == 0
+
+
+def test_slots_that_overlap_what_is_read_are_refused():
+    """Slots are written while other workgroups still read: a batch of single
+    tokens has as many slots as lengths."""
+    lib = coop.load_library()
+
+    def call(slots, table=0x100000, held=0x200000, lengths=0x300000, offsets=0x400000):
+        return lib.coop_slot_map(table, 64, 10, held, lengths, offsets, 64, 16, 8, slots, None)
+
+    for name in ("table", "held", "lengths", "offsets"):
+        assert call(0x500000, **{name: 0x500000}) == INVALID, name
+        assert call(0x500000, **{name: 0x500000 + 63 * 8}) == INVALID, name
+    assert call(0x500000, offsets=0x500000 - 64 * 8) == INVALID  # (its 65th entry)
+
+
+def test_page_tables_that_overlap_one_another_are_refused():
+    """The results of a call are apart from one another and from its workspace,
+    and status, free pages and workspace from what is read."""
+    lib = coop.load_library()
+    names = ("kind", "table", "held", "lengths", "table_out", "held_out", "kind_out", "status",
+             "free", "ws")
+
+    def call(pages=8, **ptr):
+        a = {**{n: 0x1000000 * (i + 1) for i, n in enumerate(names)}, **ptr}
+        return lib.coop_page_tables(a["kind"], pages, a["table"], 2, 4, a["held"], a["lengths"], 16, 2,
+                                    a["table_out"], a["held_out"], a["kind_out"], a["status"],
+                                    a["free"], a["ws"], 1 << 16, None)
+
+    results = ("table_out", "held_out", "kind_out", "status", "free")
+    for i, x in enumerate(results):
+        for y in results[:i]:
+            assert call(**{x: 0x20000000, y: 0x20000000}) == INVALID, (x, y)
+    for x in ("status", "free"):
+        for y in names[:4]:
+            assert call(**{x: 0x20000000, y: 0x20000000}) == INVALID, (x, y)
+    for x in names[:-1]:
+        assert call(pages=1 << 20, **{x: 0x20000000, "ws": 0x20000000}) == INVALID, x
