@@ -14,7 +14,9 @@ Caches are tensors [pages, page_size, heads, dim] of bfloat16, float16 or
 float8_e4m3fn, in any order of the first three dimensions in memory (a
 transposed view, or one half of a tensor that holds keys and values together).
 
-The operators serve a model that answers; no gradients are recorded.
+The operators serve a model that answers and have no gradients: while torch
+records them, tensors that require them are refused, and so are those that carry
+tangents.
 """
 from __future__ import annotations
 
@@ -23,8 +25,13 @@ import functools
 from typing import Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import COOP_EVICTABLE, COOP_PINNED, _check, _ptr, load_library
+
+# (torch without GPU support lacks these)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", None)
 
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float8_e4m3fn: 2}
 
@@ -43,11 +50,6 @@ class CoopRows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_uint64 * 2)]
 
 
-def _current_stream(index: int) -> int:
-    # (torch without GPU support lacks the name, so it is looked up by the call)
-    return torch._C._cuda_getCurrentRawStream(index)
-
-
 def _stream(handle: int, device):
     # (ExternalStream takes 0 for no stream and makes one)
     return torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
@@ -58,6 +60,27 @@ def _gpu(device):
         raise ValueError(f"paged pools are worked on by the GPU; tensors are on {device} "
                          "(there is no CPU fallback)")
     return device
+
+
+def _no_gradients(k, v, k_cache, v_cache, k_scale, v_scale, q=None, out=None) -> None:
+    """Refuses tensors whose gradients or tangents would be lost."""
+    recorded = torch.is_grad_enabled() and (
+        k.requires_grad or v.requires_grad or k_cache.requires_grad or v_cache.requires_grad
+        or k_scale is not None and k_scale.requires_grad
+        or v_scale is not None and v_scale.requires_grad
+        or q is not None and q.requires_grad or out is not None and out.requires_grad)
+    # (tensors carry tangents only inside of a level; -1: there is none)
+    if not recorded and getattr(forward_ad, "_current_level", 0) < 0:
+        return
+    for name, t in dict(k=k, v=v, k_cache=k_cache, v_cache=v_cache, k_scale=k_scale,
+                        v_scale=v_scale, q=q, out=out).items():
+        if t is None:
+            continue
+        if recorded and t.requires_grad:
+            raise ValueError(f"{name} requires gradients, which paged pools do not have (detach it, "
+                             "or call under torch.no_grad())")
+        if forward_ad.unpack_dual(t).tangent is not None:
+            raise ValueError(f"{name} carries a tangent, which paged pools do not pass on")
 
 
 def _vector(t: torch.Tensor, name: str, dtype, device, *shape) -> torch.Tensor:
@@ -188,7 +211,7 @@ class _Call:
             stream = _current_stream(index)
         if stream != self._home and stream not in self._met:
             self._meet(stream)
-        if torch._C._cuda_getDevice() == index:
+        if _current_device() == index:
             status = self._fn(*self._args, stream)
         else:
             with torch.cuda.device(self.device):
@@ -321,6 +344,7 @@ class CacheWrite(_Call):
             raise TypeError(f"k must be torch.bfloat16 or torch.float16, got {k.dtype}")
         if k.dim() != 3:
             raise ValueError(f"k must have shape [tokens, heads, dim], got {tuple(k.shape)}")
+        _no_gradients(k, v, k_cache, v_cache, k_scale, v_scale)
         cache = _cache(k_cache, v_cache, k_scale, v_scale, k.dtype, device)
         shape = n, _, _ = (k.shape[0], cache.heads, cache.dim)
         k_rows = _rows(k, "k", k.dtype, device, shape)
@@ -379,6 +403,7 @@ class TreeAttention(_Call):
         if q.dim() != 3 or table.dim() != 2:
             raise ValueError("q must have shape [tokens, q_heads, dim] and table [requests, "
                              f"columns], got {tuple(q.shape)} and {tuple(table.shape)}")
+        _no_gradients(k, v, k_cache, v_cache, k_scale, v_scale, q, out)
         cache = _cache(k_cache, v_cache, k_scale, v_scale, q.dtype, device)
         n, q_heads, dim = q.shape
         if cache.heads == 0 or q_heads == 0 or q_heads % cache.heads:
