@@ -487,14 +487,14 @@ struct Fp16 {
 // 95 us for 355 MB, with two.
 template <class T, bool kE4M3, uint32_t kDim, uint32_t kRowWaves>
 struct Shape {
+    static_assert(kRowWaves == 1 || kRowWaves == 2, "more rows are the wide kernel's");
     static constexpr uint32_t kGroups = 4 / kRowWaves;
-    static constexpr uint32_t kKeys = kRowWaves == 4 ? 64 : 32;  // of a tile
+    static constexpr uint32_t kKeys = 32;  // of a tile
     static constexpr uint32_t kGroupThreads = 64 * kRowWaves;
     static constexpr uint32_t kChunks = kDim / 8;  // 16-byte chunks of a row in LDS
     static constexpr uint32_t kLoads = kKeys * kChunks / kGroupThreads;      // a thread's, a tile
     static constexpr uint32_t kLoads8 = kLoads / 2;                          // with 8-bit rows
     static constexpr uint32_t kTileBytes = kKeys * kDim * 2;
-    static constexpr uint32_t kSTiles = kKeys / 32;
     static constexpr uint32_t kDTiles = kDim / 32;
     static constexpr uint32_t kBytes = kGroups * 2 * kTileBytes;
     static_assert(kLoads8 >= 1, "a thread has a load of every kind");
@@ -753,6 +753,7 @@ template <class T, bool kE4M3, uint32_t kDim, uint32_t kRowWaves>
 __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_kernel(Args a) {
     using S = Shape<T, kE4M3, kDim, kRowWaves>;
     constexpr uint32_t kKeys = S::kKeys, kLoads = S::kLoads, kLoads8 = S::kLoads8;
+    constexpr uint64_t kFull = 0xffffffffull;
     __shared__ __align__(16) uint8_t tiles[S::kBytes];
     __shared__ __align__(16) uint8_t queries[kRowWaves * kRows * kDim * 2];
     __shared__ RowAt rows_at[4][kKeys];           // one copy a wavefront
@@ -854,10 +855,8 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
             }
         }
         if (lane < kKeys) rows_at[w][my_key] = r;
-        const uint64_t all = __ballot(counts);
-        return kKeys == 64 ? all : all & 0xffffffffu;
+        return __ballot(counts) & kFull;
     };
-    constexpr uint64_t kFull = kKeys == 64 ? ~0ull : 0xffffffffull;
 
     u32x4 kreg[kLoads], vreg[kLoads];
     const uint32_t chunk = gtid % S::kChunks, row_of_load = gtid / S::kChunks;
@@ -951,30 +950,24 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
         if (more) load(tile + S::kGroups);
         if (here) {
             const bool is_new = tile >= cached_tiles;
-            f32x16 s[S::kSTiles];
+            f32x16 s;
 #pragma unroll
-            for (uint32_t t = 0; t < S::kSTiles; ++t)
-#pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) s[t][i] = 0.f;
+            for (uint32_t i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
             for (uint32_t c = 0; c < kDim / 16; ++c) {
                 const uint32_t place = (n * S::kChunks + key_chunk<kDim>(n, 2 * c + hi)) * 16;
                 const u32x4 qx = *reinterpret_cast<const u32x4*>(query_tile + place);
-#pragma unroll
-                for (uint32_t t = 0; t < S::kSTiles; ++t) {
-                    // (rows 32 apart are permuted alike)
-                    const u32x4 kx = *reinterpret_cast<const u32x4*>(key_tile + place + t * 32 * kDim * 2);
-                    s[t] = T::mfma(kx, qx, s[t]);
-                }
+                const u32x4 kx = *reinterpret_cast<const u32x4*>(key_tile + place);
+                s = T::mfma(kx, qx, s);
             }
             // which keys this lane's row sees
             uint64_t sees = counts;
             if (is_new)
                 sees = sight.of_tile<kKeys>(static_cast<int32_t>((cached_tiles + new_tiles - 1 - tile) * kKeys));
             float factor = is_new ? new_scale : cached_scale;
-            float grow = new_base<T, S::kSTiles>(s, sees, kFull, hi, &factor, &m, &l);
-            uint32_t p[S::kSTiles][8];
-            l += weights_of<T, S::kSTiles>(s, factor, m, p);
+            float grow = new_base<T, 1>(&s, sees, kFull, hi, &factor, &m, &l);
+            uint32_t p[8];
+            l += weights_of<T, 1>(&s, factor, m, &p);
             if (kE4M3 && is_new && !scaled) {
                 grow *= value_scale;
                 scaled = true;
@@ -986,26 +979,23 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
                     for (uint32_t i = 0; i < 16; ++i) o[t][i] *= grow;
             const uint32_t g = lane & 15u;
 #pragma unroll
-            for (uint32_t t = 0; t < S::kSTiles; ++t)
+            for (uint32_t half = 0; half < 2; ++half) {
+                const u32x4 px = {p[4 * half], p[4 * half + 1], p[4 * half + 2], p[4 * half + 3]};
+                const uint32_t r = 16 * half + 4 * hi + (g >> 2);
 #pragma unroll
-                for (uint32_t half = 0; half < 2; ++half) {
-                    const u32x4 px = {p[t][4 * half], p[t][4 * half + 1], p[t][4 * half + 2],
-                                      p[t][4 * half + 3]};
-                    const uint32_t r = 32 * t + 16 * half + 4 * hi + (g >> 2);
-#pragma unroll
-                    for (uint32_t dt = 0; dt < S::kDTiles; ++dt) {
-                        const uint32_t d = 32 * dt + (lane & 16u) + 4 * (g & 3u);
-                        typedef __attribute__((address_space(3))) s16x4 Lds;
-                        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
-                            value_tile + (r * S::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2));
-                        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
-                            value_tile + ((r + 8) * S::kChunks + value_chunk<kDim>(r + 8, d / 8)) * 16 +
-                            (d & 4) * 2));
-                        const uint2 a0 = __builtin_bit_cast(uint2, v0), a1 = __builtin_bit_cast(uint2, v1);
-                        const u32x4 vx = {a0.x, a0.y, a1.x, a1.y};
-                        o[dt] = T::mfma(vx, px, o[dt]);
-                    }
+                for (uint32_t dt = 0; dt < S::kDTiles; ++dt) {
+                    const uint32_t d = 32 * dt + (lane & 16u) + 4 * (g & 3u);
+                    typedef __attribute__((address_space(3))) s16x4 Lds;
+                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
+                        value_tile + (r * S::kChunks + value_chunk<kDim>(r, d / 8)) * 16 + (d & 4) * 2));
+                    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds*)(
+                        value_tile + ((r + 8) * S::kChunks + value_chunk<kDim>(r + 8, d / 8)) * 16 +
+                        (d & 4) * 2));
+                    const uint2 a0 = __builtin_bit_cast(uint2, v0), a1 = __builtin_bit_cast(uint2, v1);
+                    const u32x4 vx = {a0.x, a0.y, a1.x, a1.y};
+                    o[dt] = T::mfma(vx, px, o[dt]);
                 }
+            }
         }
         counts = next_counts;
         sync();
@@ -1017,44 +1007,42 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i) o[t][i] *= value_scale;
 
-    if constexpr (S::kGroups > 1) {
-        // join the groups: each scales its part to the common maximum and adds
-        // it to the first one's, a group after the other
-        __syncthreads();
-        if (hi == 0) {
-            joined[w][n][0] = m;
-            joined[w][n][1] = l;
-        }
-        __syncthreads();
-        float m_all = kLowest, l_all = 0.f;
-        for (uint32_t g = 0; g < S::kGroups; ++g) m_all = fmaxf(m_all, joined[g * kRowWaves + row_wave][n][0]);
-        const float base = m_all == kLowest ? 0.f : m_all;
-        for (uint32_t g = 0; g < S::kGroups; ++g)
-            l_all += joined[g * kRowWaves + row_wave][n][1] *
-                     __builtin_amdgcn_exp2f(joined[g * kRowWaves + row_wave][n][0] - base);
-        const float part = __builtin_amdgcn_exp2f(m - base);
-        // [row wave][element][lane]: every lane has the same elements in each group
-        float* const sums = reinterpret_cast<float*>(tiles) + row_wave * (kDim / 2) * 64 + lane;
-        static_assert(kRowWaves * kDim * 32 * 4 <= S::kBytes, "the sums fit where the tiles were");
-        for (uint32_t g = 1; g < S::kGroups; ++g) {
-            if (group == g)
-#pragma unroll
-                for (uint32_t t = 0; t < S::kDTiles; ++t)
-#pragma unroll
-                    for (uint32_t i = 0; i < 16; ++i) {
-                        float* const x = sums + (16 * t + i) * 64;
-                        *x = (g == 1 ? 0.f : *x) + o[t][i] * part;
-                    }
-            __syncthreads();
-        }
-        if (group != 0) return;
-#pragma unroll
-        for (uint32_t t = 0; t < S::kDTiles; ++t)
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) o[t][i] = o[t][i] * part + sums[(16 * t + i) * 64];
-        m = m_all;
-        l = l_all;
+    // join the groups: each scales its part to the common maximum and adds
+    // it to the first one's, a group after the other
+    __syncthreads();
+    if (hi == 0) {
+        joined[w][n][0] = m;
+        joined[w][n][1] = l;
     }
+    __syncthreads();
+    float m_all = kLowest, l_all = 0.f;
+    for (uint32_t g = 0; g < S::kGroups; ++g) m_all = fmaxf(m_all, joined[g * kRowWaves + row_wave][n][0]);
+    const float base = m_all == kLowest ? 0.f : m_all;
+    for (uint32_t g = 0; g < S::kGroups; ++g)
+        l_all += joined[g * kRowWaves + row_wave][n][1] *
+                 __builtin_amdgcn_exp2f(joined[g * kRowWaves + row_wave][n][0] - base);
+    const float part = __builtin_amdgcn_exp2f(m - base);
+    // [row wave][element][lane]: every lane has the same elements in each group
+    float* const sums = reinterpret_cast<float*>(tiles) + row_wave * (kDim / 2) * 64 + lane;
+    static_assert(kRowWaves * kDim * 32 * 4 <= S::kBytes, "the sums fit where the tiles were");
+    for (uint32_t g = 1; g < S::kGroups; ++g) {
+        if (group == g)
+#pragma unroll
+            for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+                for (uint32_t i = 0; i < 16; ++i) {
+                    float* const x = sums + (16 * t + i) * 64;
+                    *x = (g == 1 ? 0.f : *x) + o[t][i] * part;
+                }
+        __syncthreads();
+    }
+    if (group != 0) return;
+#pragma unroll
+    for (uint32_t t = 0; t < S::kDTiles; ++t)
+#pragma unroll
+        for (uint32_t i = 0; i < 16; ++i) o[t][i] = o[t][i] * part + sums[(16 * t + i) * 64];
+    m = m_all;
+    l = l_all;
     write_row<T, kDim, kKeys>(a, item, e, place, sight, odd, hi, o, m, l);
 }
 
