@@ -360,7 +360,8 @@ coop_status_t coop_replay(uint64_t *size, uint64_t *cost, uint8_t *kind, uint32_
  * hold) are read; table_out, held_out and kind_out are written.  Each of the
  * three may be its input (the update is then in place) or must not overlap
  * any input, and no output or workspace overlaps another.  A page is in one row
- * at most.
+ * at most, and one that is in a row is not free: pages that are to be evicted
+ * leave their rows by a shorter length here, not by a change of kind[].
  *
  * A sequence of n tokens needs ceil(n / page_size) pages.
  *  1. Rows that hold more than they need give back their last pages: these

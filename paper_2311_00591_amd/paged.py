@@ -239,7 +239,9 @@ class PageTables(_Call):
     to hold.  Rows that hold more pages than ceil(length / page_size) give their
     last ones back; then rows that need more take the lowest free pages, in the
     rows' order, which become `taken`.  Once a row cannot have all that it
-    needs, it and every later one that needs more keep what they had.
+    needs, it and every later one that needs more keep what they had.  A page
+    that a row names must not be set free in `kind` by hand: what is to be
+    evicted leaves its row by a shorter length.
 
     Results: `table`, `held`, `kind` (new tensors; with out=(table, held, kind)
     written there, and these may be the inputs themselves), `status` (int32
