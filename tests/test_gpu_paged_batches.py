@@ -1,12 +1,16 @@
-"""Batches as a server has them."""
+"""Batches as a server has them: single tokens beside a long piece of a prompt,
+and pages that the window search takes back from sequences."""
 import sys
 
 import numpy as np
 import pytest
 
+import paged_reference as ref
+
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+BF16, E4M3 = torch.bfloat16, torch.float8_e4m3fn
 DEV = "cuda"
 
 
@@ -22,6 +26,54 @@ def _announce(label):
 
 def _ints(a, dtype=torch.int64):
     return torch.tensor(np.asarray(a), device=DEV).to(dtype)
+
+
+@pytest.mark.parametrize("counts, at, cache", [
+    ([1] * 63 + [1024], 63, BF16),     # the mean calls for wide tiles: single tokens on them
+    ([1] * 255 + [2048], 100, BF16),   # and for narrow ones: a prompt on them
+    ([1] * 40 + [700], 0, E4M3), ([1] * 7 + [900], 3, E4M3), ([1, 1, 1, 3000], 3, BF16)])
+def test_a_prompt_among_single_tokens(counts, at, cache):
+    """Every row is within what rounding allows (a few of the prompt's, all of
+    the single tokens), wherever the prompt stands."""
+    coop = _coop()
+    n = len(counts)
+    counts = counts[:-1][:at] + counts[-1:] + counts[:-1][at:]
+    _announce(f"attention, {n - 1} single tokens and a piece of {max(counts)}, {cache}")
+    rng = np.random.default_rng(n)
+    q_heads, heads, dim, page = 8, 2, 128, 16
+    lengths = rng.integers(1, 200, n)
+    held = -(-lengths // page)
+    pages = int(held.sum()) + 1
+    g = torch.Generator().manual_seed(n)
+    pool = [torch.randn((pages, page, heads, dim), generator=g) for _ in "kv"]
+    scales = [None, None]
+    if cache == E4M3:
+        scales = [torch.full((heads,), 0.01), torch.full((heads,), 0.02)]
+        pool = [x / s[:, None] for x, s in zip(pool, scales)]
+        scales = [s.to(DEV) for s in scales]
+    k_cache, v_cache = (x.to(cache).to(DEV) for x in pool)
+    table = np.full((n, int(held.max())), -1)
+    order = rng.permutation(pages)
+    for b, h in enumerate(held):
+        table[b, :h], order = order[:h], order[h:]
+    total = sum(counts)
+    q, k, v = (torch.randn((total, h, dim), generator=g).to(DEV, BF16) for h in (q_heads, heads, heads))
+    table, lengths = _ints(table, torch.int32), _ints(lengths)
+    offsets = np.concatenate([[0], np.cumsum(counts)])
+    got = coop.tree_attention(q, k, v, k_cache, v_cache, table, lengths, _ints(offsets),
+                              k_scale=scales[0], v_scale=scales[1])
+    for b, c in enumerate(counts):
+        pick = [0] if c == 1 else [0, 1, c // 2, c - 1]
+        lo, hi = offsets[b], offsets[b + 1]
+        want, tol = ref.attention(q[lo:hi], k[lo:hi], v[lo:hi], k_cache, v_cache, table[b:b + 1],
+                                  lengths[b:b + 1], _ints([0, c]), None, dim ** -0.5, scales[0],
+                                  scales[1], only=pick)
+        mine, want, tol = got[lo:hi].double().cpu().numpy()[pick], want[pick], tol[pick]
+        # (a few of the pool's numbers are past e4m3's range, and not numbers there)
+        assert np.array_equal(np.isnan(mine), np.isnan(want))
+        fine = ~np.isnan(want)
+        worst = (np.abs(mine - want)[fine] / tol[fine]).max()
+        assert worst <= 1, (b, worst)
 
 
 def test_pages_that_are_evicted_leave_their_rows():
