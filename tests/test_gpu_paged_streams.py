@@ -225,3 +225,22 @@ def test_inputs_are_kept_for_the_stream_that_reads_them(busy):
     torch.cuda.synchronize()
     for cache, x in ((k_cache, k), (v_cache, v)):
         assert torch.equal(cache.view(128, 8, 128)[64:], x[picked]) and not cache[:4].any()
+
+
+def test_empty_calls_on_another_stream():
+    """Tensors without memory have none to wait for or to keep."""
+    coop = _coop()
+    _announce("empty calls on another stream")
+    a = _attention()
+    side = torch.cuda.Stream()
+    stream = side.cuda_stream
+    none = {**a, **{n: a[n][:0] for n in "qkv"}, "token_offsets": a["token_offsets"] * 0}
+    assert coop.tree_attention(**none, stream=stream).shape == (0, 8, 128)
+    empty = torch.zeros(0, dtype=torch.int64, device=DEV)
+    coop.cache_write(a["k"][:0], a["v"][:0], empty, a["k_cache"], a["v_cache"], stream=stream)
+    assert coop.slot_map(a["table"], a["lengths"].int(), a["lengths"], a["token_offsets"], 0, 16, 40,
+                         stream=stream).shape == (0,)
+    got = coop.page_tables(torch.zeros(3, dtype=torch.uint8, device=DEV), a["table"][:0, :0],
+                           empty.int(), empty, 16, stream=stream)
+    side.synchronize()
+    assert (got[3].item(), got[4].item()) == (0, 3)
