@@ -16,10 +16,10 @@
 //     of free pages: nothing is listed or sorted, each page finds its own row.
 //
 // What bounds it.  A small pool is a chain of some ten dependent steps of one
-// workgroup: 6.5 us for 8 sequences on 600 pages, 19 us for 512 on 107 thousand
-// (4.9 MB in all).  A large one is four launches, each with its start and its
-// searches: 2.5, 7.9, 5.8 and 11.8 us for 4096 sequences on 772 thousand pages,
-// where 44 MB are moved, 9 us at the rate of a large copy.
+// workgroup: 6.5 us for 8 sequences on 406 pages, 18 us for 512 on 107 thousand
+// (2.6 MB in all).  A large one is four launches, each with its start and its
+// searches: 3.4, 8.0, 5.9 and 11.9 us for 4096 sequences on 772 thousand pages,
+// where 21 MB are read and written, 4.2 us at the rate of a large copy.
 //
 // coop_slot_map and coop_cache_write are one launch each.
 
@@ -655,7 +655,7 @@ struct WriteArgs {
 // A thread takes a chunk (eight elements) of a token's key row and the same of
 // its value row; consecutive threads take consecutive chunks.  Memory bounds it:
 // 65536 tokens of 8 heads of 128 into an e4m3 pool, 383 MB, take 84.6 us (4.5
-// TB/s), 64 tokens 2.7 us.  Divisions of 64 bits and by the scales took 109 us.
+// TB/s), 64 tokens 2.9 us.  Divisions of 64 bits and by the scales took 109 us.
 template <bool kE4M3>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(WriteArgs a) {
     const coop_cache_t& cache = a.cache;
@@ -726,7 +726,9 @@ struct TablesLayout {
 // 512 rows on 107 thousand pages 25 : 35.  Launched ahead, so that only the
 // device counts: 8 rows 11 : 17, 256 rows on 54 thousand pages 21 : 24, 512
 // rows 25 : 25, and 36 : 26 where a third of them give back all that they hold,
-// which one workgroup has to read; 1000 such rows 50 : 33.
+// which one workgroup has to read; 1000 such rows 50 : 33.  So 512 rows are where
+// the device is even; calls from a host gain there, replays of a batch in which
+// many sequences end lose.
 bool is_small(uint64_t pages, uint64_t rows) { return pages <= kSmallPages && rows <= kSmallRows; }
 
 TablesLayout tables_layout(uint64_t pages, uint64_t rows) {

@@ -13,13 +13,13 @@
 // G T rows, 4 dim products each: below about 250 rows the pool's bytes
 // bound the call, above that the matrix instructions.  Measured, 32 query
 // heads over 8 of 128 dims, 16-bit:
-//   64 single tokens over 500 to 16000 cached ones   234 us, 5.1 TB/s
-//   8 tokens over 260 thousand (64 heads over 8)     205 us, 5.2 TB/s
-//   16 trees of 64 over 1000 to 8000                 112 us, 2.2 TB/s, 515 TFLOP/s
+//   64 single tokens over 500 to 16000 cached ones   239 us, 5.0 TB/s
+//   8 tokens over 260 thousand (64 heads over 8)     210 us, 5.1 TB/s
+//   16 trees of 64 over 1000 to 8000                 113 us, 2.2 TB/s, 513 TFLOP/s
 //   4 pieces of prompts, 1000 to 2048 tokens over
-//   none to 12000                                    388 us, 763 TFLOP/s
-// where a copy of 2 GiB reaches 4.9 TB/s and a large product of matrices 1250
-// TFLOP/s.
+//   none to 12000                                    403 us, 734 TFLOP/s
+// where a copy of 2 GiB reaches 4.9 TB/s, reading alone 6.3 and a large product
+// of matrices 1250 TFLOP/s.
 //
 // The work.  A workgroup takes an item: row tile rt of one request and head,
 // and a range of its keys.  Up to 64 rows, four wavefronts take it
@@ -1060,14 +1060,15 @@ __global__ __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) void tree_attention_
 // needed, and every product then waits for LDS).  8-bit tiles stay 8-bit in LDS
 // and become operands as they are read.
 //
-// Four pieces of prompts (above) take 388 us, 763 TFLOP/s; a SIMD's matrix unit
+// Four pieces of prompts (above) take 403 us, 734 TFLOP/s; a SIMD's matrix unit
 // is busy 38 % of the time and its vector unit 44 %, seldom at once.  Taking the
 // scores of the next tile ahead of the softmax needs more registers than there
-// are (760 us, spilled); two sets of wavefronts that take turns, one at the
-// products while the other weighs, came to 391 us and cost the other calls here
-// 3 to 10 %.  The lambdas are inlined by force, which decides what stays in
-// registers (64 trees of 32 tokens, heads of 256: 291 us for 310).  48 trees of
-// 1 to 40 tokens over e4m3 take 108 us: 1.6 TB/s, 340 TFLOP/s.
+// are (twice the time, spilled); two sets of wavefronts that take turns, one at
+// the products while the other weighs, took 391 us where this took 388 and cost
+// the other calls here 3 to 10 %.  The lambdas are inlined by force, which
+// decides what stays in registers (64 trees of 32 tokens, heads of 256: 291 us
+// for 310).  48 trees of 1 to 40 tokens over e4m3 take 111 us: 1.6 TB/s, 330
+// TFLOP/s.
 template <bool kE4M3, uint32_t kDim, uint32_t kWaves>
 struct Wide {
     static constexpr uint32_t kKeys = kDim == 256 ? 32 : 64;
@@ -1433,7 +1434,7 @@ __global__ __launch_bounds__(64 * kWaves, kDim == 256 ? 1 : 2) void tree_attenti
 // Joins the parts of rows whose keys were cut.  A row's parts are dealt to
 // kWaves wavefronts: four (a workgroup a row) where there are few rows and so
 // many parts, one where there are many rows.  Reading the parts bounds it (19
-// us of the 112 for 16 trees of 64 tokens, 66 MB; 4 us for four short
+// us of the 113 for 16 trees of 64 tokens, 66 MB; 4 us for four short
 // sequences).  With four or one wavefront a row, the whole call: one token over
 // 16000 cached ones 24.4 : 26.3 us, 16 trees of 64 137 : 114.
 template <class T, uint32_t kDim, uint32_t kWaves>
@@ -1539,7 +1540,11 @@ struct Plan {
 
 // The wavefronts that share every tile of keys, 32 rows each: as many as the
 // rows of an average request fill.  The lengths are on the device, the average
-// is all that the host knows of them.
+// is all that the host knows of them.  A batch of unlike requests has the
+// average's tiles for all: 255 single tokens over 500 to 4000 with a piece of
+// 2048 over 2000 (36 rows on average, two wavefronts) take 605 us, the two as
+// calls of their own 362 and 153; 63 over 500 to 16000 with a piece of 1024 (68
+// rows, four) 315 us, apart 233 and 81.
 //
 // Measured with 64 requests of 200 to 4000 cached tokens, 32 query heads over 8
 // of 128 dims in bf16 (us, the fewer wavefronts first):
