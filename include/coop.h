@@ -439,7 +439,7 @@ typedef struct {
 } coop_cache_t;
 
 /* Rows of tokens: the row of a token and head starts at token * stride[0] +
- * head * stride[1] elements (the same rules of alignment as above). */
+ * head * stride[1] elements (the same rules as above). */
 typedef struct {
     const void *data;
     uint64_t stride[2];

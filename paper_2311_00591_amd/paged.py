@@ -50,6 +50,7 @@ class CoopRows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_uint64 * 2)]
 
 
+@functools.lru_cache(maxsize=64)
 def _stream(handle: int, device):
     # (ExternalStream takes 0 for no stream and makes one)
     return torch.cuda.ExternalStream(handle, device) if handle else torch.cuda.default_stream(device)
@@ -193,7 +194,9 @@ class _Call:
             # (the default stream, 0, is never captured)
             if not (self._home and _capturing(home)):
                 return
-        other.wait_stream(home)
+            other.wait_stream(home)
+        elif not home.query():  # (asking is far cheaper than waiting for what is done)
+            other.wait_stream(home)
         for t in self._tensors:
             if t is not None:
                 t.record_stream(other)

@@ -23,7 +23,7 @@ def _announce(label):
 
 @pytest.fixture(scope="module")
 def busy():
-    """Enqueues some 50 ms of products on the current stream; returns an event
+    """Enqueues some 150 ms of products on the current stream; returns an event
     behind them."""
     a = torch.zeros((8192, 8192), dtype=BF16, device=DEV)
     out = torch.empty_like(a)
@@ -38,7 +38,7 @@ def busy():
     start = time.perf_counter()
     enqueue(20).synchronize()
     took = (time.perf_counter() - start) / 20
-    return lambda: enqueue(int(0.05 / took) + 1)
+    return lambda: enqueue(int(0.15 / took) + 1)
 
 
 def _attention():
