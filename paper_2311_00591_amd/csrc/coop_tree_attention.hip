@@ -17,7 +17,8 @@
 //   8 tokens over 260 thousand (64 heads over 8)     210 us, 5.1 TB/s
 //   16 trees of 64 over 1000 to 8000                 113 us, 2.2 TB/s, 513 TFLOP/s
 //   4 pieces of prompts, 1000 to 2048 tokens over
-//   none to 12000                                    403 us, 734 TFLOP/s
+//   none to 12000                                    403 us, 734 TFLOP/s (393 to
+//   429 from one machine to another)
 // where a copy of 2 GiB reaches 4.9 TB/s, reading alone 6.3 and a large product
 // of matrices 1250 TFLOP/s.
 //
